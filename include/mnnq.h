@@ -302,6 +302,107 @@ int mnnq_debug_set(const char *key, const char *value);
  * out8: HOST pointer to 8 int32.  Same shape / mode errors as the calls themselves. */
 int mnnq_plan_debug(int what, int64_t M, int64_t N, int64_t K, int group, int mode, int32_t *out8);
 
+/* ---- Attention between the q|k|v and the output projection -------------------------------------
+ *
+ * Four calls: attention over a whole prompt (mnnq_attn_prefill), appending keys and values to a cache
+ * of 8-bit codes (mnnq_kv_append; Section 4.2 quantizes the cache: keys int4 / int8, values fp8),
+ * attention of one or a few tokens over that cache (mnnq_attn_decode), and dropping the tokens that had
+ * the least attention (mnnq_kv_evict).
+ *
+ * Rows.  q, k, v and out hold one row of head_dim 16-bit values per token and head; consecutive values
+ * of a row are adjacent, `..._token` and `..._head` are the distances in elements from a token's, a head's
+ * row to the next one's (the column ranges of a q|k|v projection's result [tokens, N] have token distance N
+ * and head distance head_dim).  Both distances are multiples of 8, and arrays 16-byte aligned.
+ * Heads.  heads is a multiple of kv_heads; query head h reads key and value head h / (heads / kv_heads).
+ * head_dim: a multiple of 16, 16 to 256.  scale: the factor of q . k (usually 1 / sqrt(head_dim)), finite
+ * and above zero.
+ * A query that no key is visible to gives a row of zeros.  Softmax statistics and sums are fp32; the
+ * probabilities enter the second product rounded to the type of its other operand (prompt: `type`,
+ * cache: fp16 with 2^-39 the smallest that counts), the result is rounded once.
+ * A NaN or an infinity in q, k or v reaches the rows that see it and no other row.
+ * Device arrays of indices are not looked at on the host; what they hold is bounded in the kernels: a
+ * sequence's start and end are clamped to the number of rows given (an end before its start is an empty
+ * sequence), lengths to 0 and what the table has room for; tokens in blocks outside the cache's are
+ * neither read nor written, and count as masked. */
+
+/* Type of q, k, v and out. */
+typedef enum { MNNQ_F16 = 0, MNNQ_BF16 = 1 } mnnq_type;
+
+/* Codes of the cache: a code c of a block and head with range r stands for c * r / 127 (int8, -127..127) or
+ * c * r / 448 (fp8: e4m3, 448 its largest number).  r is the greatest magnitude appended to that block and
+ * head, so it is a number of `type` exactly; a new value x gets the code round(x * 127 / r), resp. the e4m3
+ * number nearest to x * 448 / r, ties to even; a range of zero has codes of zero.  An infinity or a NaN
+ * makes the range infinite or NaN, and what its block and head hold undefined (no error, no effect on
+ * other blocks and heads). */
+typedef enum { MNNQ_KV_INT8 = 0, MNNQ_KV_FP8 = 1 } mnnq_kv_form;
+
+/* A cache, and the sequences in it.  A HOST structure of device pointers; calls read it before they return.
+ * Token t of sequence s is token t % block_tokens of block block_table[s * table_blocks + t / block_tokens];
+ * blocks are the caller's to give out, no two sequences may append to the same one.  Entries of the table
+ * behind a sequence's last token are not read. */
+typedef struct {
+    void *k_codes, *v_codes;        /* [blocks, kv_heads, block_tokens, head_dim], one byte each, 16-byte aligned */
+    float *k_range, *v_range;       /* [blocks, kv_heads] */
+    const int32_t *block_table;     /* [sequences, table_blocks] */
+    const int32_t *lengths;         /* [sequences]: tokens in the cache (mnnq_kv_append: before the new ones) */
+    int64_t blocks, sequences, table_blocks;
+    int32_t kv_heads, head_dim;
+    int32_t block_tokens;           /* 16, 32, 64 or 128 */
+    int32_t k_form, v_form;         /* mnnq_kv_form */
+} mnnq_kv_cache;
+
+/* Causal attention over packed prompts: sequence s has the queries q_start[s] .. q_start[s + 1] of the
+ * q_tokens rows of q and out, and the keys k_start[s] .. k_start[s + 1] of the k_tokens rows of k and v.
+ * The last query sees all keys of its sequence, each one before it one key less:
+ *   out_i = sum_{j <= i + keys - queries} softmax_j(scale q_i . k_j) v_j.
+ * Rows of out that belong to no sequence are not written.
+ * q_start, k_start: int32 [sequences + 1], not falling; they may be the same array. */
+int mnnq_attn_prefill(int type, int64_t sequences, const int32_t *q_start, const int32_t *k_start,
+                      int64_t q_tokens, int64_t k_tokens, int heads, int kv_heads, int head_dim, float scale,
+                      const void *q, int64_t q_token, int64_t q_head, const void *k, int64_t k_token, int64_t k_head,
+                      const void *v, int64_t v_token, int64_t v_head, void *out, int64_t out_token, int64_t out_head,
+                      void *stream);
+
+/* Quantizes new rows of k and v and appends them to the cache; cache->lengths are the lengths before (the
+ * call leaves them as they are).  start: int32 [sequences + 1], sequence s appends rows start[s] ..
+ * start[s + 1] of the `tokens` rows; NULL: every sequence appends tokens / sequences rows (tokens must be a
+ * multiple of sequences).  Where a block already holds tokens and the new ones raise its range from r to r',
+ * the codes of the older tokens become round(c * r / r') (fp8: the nearest number).  Tokens beyond
+ * table_blocks * block_tokens are dropped. */
+int mnnq_kv_append(const mnnq_kv_cache *cache, int type, const int32_t *start, int64_t tokens,
+                   const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+                   void *stream);
+
+/* Attention over the cache: `tokens` queries for each sequence, rows s * tokens + t of q and out, which are
+ * the queries of the last `tokens` tokens in the cache - query t of sequence s sees the tokens below
+ * lengths[s] - tokens + t + 1.  max_length: an upper bound of the lengths (0: the room of the table); longer
+ * sequences are cut to their first max_length tokens.  The work is laid out for max_length, so that one not
+ * far above the longest length is the fastest.
+ * weights: NULL, or fp32 [sequences, kv_heads, weights_stride], weights_stride >= the bound: the attention
+ * given to token j by all queries that share the head, sum_{queries, heads of the group} softmax_j, is added
+ * to weights[s, h, j].
+ * workspace: mnnq_attn_decode_workspace_size() bytes, 16-byte aligned, scratch; calls sharing one must not
+ * overlap in time.  NULL where the size is 0. */
+size_t mnnq_attn_decode_workspace_size(const mnnq_kv_cache *cache, int64_t tokens, int heads, int64_t max_length,
+                                       int with_weights);
+int mnnq_attn_decode(const mnnq_kv_cache *cache, int type, int64_t tokens, int heads, int64_t max_length, float scale,
+                     const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,
+                     float *weights, int64_t weights_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Keeps, of every sequence and key head by itself, the last `recent` tokens and those of the others with the
+ * greatest weights (among equal ones the earlier; NaN counts as greatest), min(keep, length) in all, and
+ * writes them, in their order, to the blocks of new_table [sequences, new_table_blocks] of the same cache.
+ * Those blocks must not be among the blocks the sequences hold now, which afterwards are free.
+ * weights: fp32 [sequences, kv_heads, weights_stride], as mnnq_attn_decode adds them up.
+ * A new block's range is the greatest range that its tokens' blocks had; codes are rounded to it.
+ * kept: int32 [sequences, kv_heads, keep], the kept tokens' old places, -1 behind the last; new_lengths:
+ * int32 [sequences]; new_weights: fp32 [sequences, kv_heads, new_weights_stride], the kept tokens' weights,
+ * zeros behind the last (stride >= keep; the room behind is for the tokens to come).  recent <= keep;
+ * new_table_blocks * block_tokens >= keep, or new lengths are cut to that room. */
+int mnnq_kv_evict(const mnnq_kv_cache *cache, const float *weights, int64_t weights_stride, int64_t keep, int64_t recent,
+                  const int32_t *new_table, int64_t new_table_blocks, int32_t *kept, int32_t *new_lengths,
+                  float *new_weights, int64_t new_weights_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

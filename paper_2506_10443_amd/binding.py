@@ -27,6 +27,7 @@ NATIVE_8BIT = 32        # flag for MODE_W8_MIN_FLOAT: the codes as bytes q8 - 12
 try:
     # names, arguments and defaults: help(mnnq_linear_decode_fused) etc.
     from ._native import (  # noqa: F401
+        mnnq_attn_decode, mnnq_attn_prefill, mnnq_kv_append, mnnq_kv_evict,
         mnnq_linear_decode, mnnq_linear_decode_f16, mnnq_linear_decode_f16_o16, mnnq_linear_decode_fused,
         mnnq_linear_decode_fused_o16, mnnq_linear_decode_o16, mnnq_linear_prefill, mnnq_linear_prefill_f16,
         mnnq_linear_prefill_f16_o16, mnnq_linear_prefill_fused, mnnq_linear_prefill_fused_o16,
@@ -44,7 +45,8 @@ except ImportError as _e:
     for _name in ("mnnq_linear_decode", "mnnq_linear_decode_f16", "mnnq_linear_decode_f16_o16", "mnnq_linear_decode_fused",
                   "mnnq_linear_decode_fused_o16", "mnnq_linear_decode_o16", "mnnq_linear_prefill",
                   "mnnq_linear_prefill_f16", "mnnq_linear_prefill_f16_o16", "mnnq_linear_prefill_fused",
-                  "mnnq_linear_prefill_fused_o16", "mnnq_linear_prefill_o16", "mnnq_pack_weights"):
+                  "mnnq_linear_prefill_fused_o16", "mnnq_linear_prefill_o16", "mnnq_pack_weights", "mnnq_attn_decode", "mnnq_attn_prefill",
+                  "mnnq_kv_append", "mnnq_kv_evict"):
         globals()[_name] = _missing(_name)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -61,7 +63,17 @@ EXPORTS = (
     "mnnq_linear_prefill_fused_static", "mnnq_static_scratch_bytes",
     "mnnq_linear_acc_debug_planes", "mnnq_debug_set",
     "mnnq_act_planes", "mnnq_linear_prefill_planes", "mnnq_act_planes_size",
+    "mnnq_attn_prefill", "mnnq_kv_append", "mnnq_attn_decode", "mnnq_attn_decode_workspace_size", "mnnq_kv_evict",
 )
+
+
+class KvCache(ctypes.Structure):
+    """mnnq_kv_cache of the C-ABI."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_range", ctypes.c_void_p),
+                ("v_range", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("blocks", ctypes.c_int64), ("sequences", ctypes.c_int64), ("table_blocks", ctypes.c_int64),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("k_form", ctypes.c_int32), ("v_form", ctypes.c_int32)]
 
 
 class MnnqError(RuntimeError):
@@ -72,6 +84,7 @@ class MnnqError(RuntimeError):
 
 
 _lib = None
+FAKE = 16     # an address where a size query only wants one that is there and aligned
 
 
 def lib() -> ctypes.CDLL:
@@ -119,6 +132,13 @@ def lib() -> ctypes.CDLL:
         L.mnnq_act_planes_size.restype = sz
         L.mnnq_act_planes_size.argtypes = [i64, i64, i32]
         L.mnnq_static_scratch_bytes.restype = sz
+        f32, cache = ctypes.c_float, ctypes.POINTER(KvCache)
+        L.mnnq_attn_prefill.argtypes = [i32, i64, vp, vp, i64, i64, i32, i32, i32, f32] + 4 * [vp, i64, i64] + [vp]
+        L.mnnq_kv_append.argtypes = [cache, i32, vp, i64] + 2 * [vp, i64, i64] + [vp]
+        L.mnnq_attn_decode.argtypes = [cache, i32, i64, i32, i64, f32] + 2 * [vp, i64, i64] + [vp, i64, vp, sz, vp]
+        L.mnnq_attn_decode_workspace_size.restype = sz
+        L.mnnq_attn_decode_workspace_size.argtypes = [cache, i64, i32, i64, i32]
+        L.mnnq_kv_evict.argtypes = [cache, vp, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp]
         L.mnnq_static_scratch_bytes.argtypes = []
         _lib = L
     return _lib
@@ -283,6 +303,15 @@ def mnnq_linear_prefill_fused_static(packed, N: int, K: int, x, bias=None, out=N
     _check(lib().mnnq_linear_prefill_fused_static(_ptr(packed), M, N, K, GROUP, mode, _ptr(x), _ptr(bias), _ptr(y),
                                                   _stream()), "mnnq_linear_prefill_fused_static")
     return y
+
+
+def mnnq_attn_decode_workspace_size(q, k_codes, block_table, max_length: int = 0, weights: bool = False) -> int:
+    """Bytes of scratch mnnq_attn_decode needs for these arrays (their shapes and types are looked at)."""
+    S, blocks = block_table.shape
+    c = KvCache(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, k_codes.shape[0], S, blocks, k_codes.shape[1], k_codes.shape[3],
+                k_codes.shape[2], 0, 0)
+    return int(lib().mnnq_attn_decode_workspace_size(ctypes.byref(c), q.shape[0] // max(S, 1), q.shape[1], max_length,
+                                                     int(weights)))
 
 
 def mnnq_static_scratch_bytes() -> int:

@@ -1,0 +1,239 @@
+"""mnnq_kv_append and mnnq_kv_evict: codes, ranges and places are those of the definition, exactly."""
+import pytest
+import torch
+
+import attn_reference as R
+from paper_2506_10443_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+I8, F8 = torch.int8, torch.float8_e4m3fn
+
+
+class Pair:
+    """The same cache on the GPU and in 64 bits; blocks given out in a random order."""
+
+    def __init__(self, sequences, table_blocks, kv_heads, block, dim, k_type=I8, v_type=F8, seed=0, spare=0):
+        gen = torch.Generator().manual_seed(seed)
+        blocks = sequences * table_blocks + spare + 2
+        order = torch.randperm(blocks, generator=gen).to(torch.int32)
+        self.table = order[:sequences * table_blocks].view(sequences, table_blocks)
+        self.free = order[sequences * table_blocks:sequences * table_blocks + spare]
+        self.ref = R.Cache(blocks, kv_heads, block, dim, k_type, v_type)
+        self.gpu = {}
+        for x, t in (("k", k_type), ("v", v_type)):
+            # what blocks hold that nobody has written yet: anything, NaN codes and ranges among it
+            self.gpu[x + "_codes"] = torch.full((blocks, kv_heads, block, dim), 0x7f, dtype=torch.uint8, device="cuda").view(t)
+            self.gpu[x + "_range"] = torch.full((blocks, kv_heads), float("nan"), device="cuda")
+        self.lengths = [0] * sequences
+
+    def args(self, lengths=None, table=None):
+        return (self.gpu["k_codes"], self.gpu["k_range"], self.gpu["v_codes"], self.gpu["v_range"],
+                (self.table if table is None else table).cuda(),
+                torch.tensor(self.lengths if lengths is None else lengths, dtype=torch.int32, device="cuda"))
+
+    def append(self, k, v, counts):
+        uniform = len(set(counts)) == 1
+        start = None
+        at = [0]
+        for n in counts:
+            at.append(at[-1] + n)
+        if not uniform:
+            start = torch.tensor(at, dtype=torch.int32, device="cuda")
+        B.mnnq_kv_append(k.cuda(), v.cuda(), *self.args(), start=start)
+        for s, n in enumerate(counts):
+            if n:
+                self.ref.append("k", self.table[s], self.lengths[s], k[at[s]:at[s + 1]])
+                self.ref.append("v", self.table[s], self.lengths[s], v[at[s]:at[s + 1]])
+            self.lengths[s] += n
+
+    def check(self, tables=None, lengths=None):
+        """Codes of the tokens that are there, ranges of their blocks."""
+        tables, lengths = self.table if tables is None else tables, self.lengths if lengths is None else lengths
+        block = self.ref.block
+        for x in "kv":
+            codes = self.gpu[x + "_codes"].view(torch.uint8).cpu().view(self.ref.type[x]).double()
+            ranges = self.gpu[x + "_range"].cpu().double()
+            for s, n in enumerate(lengths):
+                for b in range(-(-n // block)):
+                    at, used = int(tables[s][b]), min(block, n - b * block)
+                    assert torch.equal(ranges[at], self.ref.range[x][at]), (x, s, b)
+                    assert torch.equal(codes[at, :, :used], self.ref.codes[x][at, :, :used]), (x, s, b)
+
+
+def rows(gen, tokens, heads, dim, dtype, spread=1.0):
+    x = torch.randn((tokens, heads, dim), generator=gen) * spread
+    return (x * torch.exp(torch.randn((tokens, 1, 1), generator=gen))).to(dtype)
+
+
+@pytest.mark.parametrize("k_type,v_type", [(I8, I8), (I8, F8), (F8, I8), (F8, F8)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim,block", [(128, 64), (64, 16), (80, 32), (256, 128), (16, 16)])
+def test_tokens_one_by_one_and_in_prompts(k_type, v_type, dtype, dim, block):
+    gen = torch.Generator().manual_seed(dim)
+    c = Pair(3, 8, 2, block, dim, k_type, v_type)
+    print("append", k_type, v_type, dtype, dim, block, flush=True)
+    for counts in ([5, 1, block], [1, 1, 1], [1, 1, 1], [0, 2 * block + 3, 7], [block - 7, 1, 1], [1, 1, 1], [3, 3, 3]):
+        n = sum(counts)
+        c.append(rows(gen, n, 2, dim, dtype), rows(gen, n, 2, dim, dtype), counts)
+        c.check()
+
+
+def test_ranges_that_grow_round_the_older_codes():
+    c = Pair(1, 1, 1, 16, 16, I8, F8)
+    k = torch.zeros(16, 1, 16, dtype=torch.float16)
+    for i in range(16):
+        k[i, 0] = torch.arange(16) * (0.37 if i % 3 else 1.0) * (1 + i)
+        c.append(k[i:i + 1], -k[i:i + 1], [1])
+        c.check()
+
+
+def test_zeros_ties_and_extremes():
+    c = Pair(1, 4, 1, 16, 16, I8, F8)
+    k = torch.zeros(64, 1, 16, dtype=torch.bfloat16)
+    k[16:32] = (torch.arange(256).view(16, 1, 16) - 127.0) / 2     # half steps of a range of 64.5, 254 (ties)
+    k[31, 0, 15] = 254.0
+    k[32:48] = 3.0e38                                              # near the greatest number
+    k[48:64] = 1.0e-39                                             # below the least normal one
+    c.append(k, k, [64])
+    c.check()
+
+
+def test_half_way_codes():
+    """Greatest magnitudes of which every half is a tie: 127 and its doubles, and halves of any range."""
+    for top in (127.0, 254.0, 1.0, 1.25, 96.5):
+        c = Pair(1, 1, 1, 16, 64, I8, F8)
+        k = (torch.arange(16 * 64).view(16, 1, 64) % 255 - 127).float() * 0.5 * (top / 127)
+        k[0, 0, :4] = torch.tensor([top, top / 2, -top / 2, top / 4])
+        c.append(k.half(), k.half(), [16])
+        c.check()
+
+
+def test_strided_rows():
+    gen = torch.Generator().manual_seed(3)
+    whole = rows(gen, 40, 8, 64, torch.float16).cuda()
+    c = Pair(1, 3, 2, 16, 64)
+    B.mnnq_kv_append(whole[:, 4:6], whole[:, 6:], *c.args())
+    host = whole.cpu()
+    c.ref.append("k", c.table[0], 0, host[:, 4:6])
+    c.ref.append("v", c.table[0], 0, host[:, 6:])
+    c.lengths = [40]
+    c.check()
+
+
+def test_tokens_without_a_place_are_dropped():
+    """Past the table's room, in blocks that the cache does not have, and lengths that are no lengths."""
+    gen = torch.Generator().manual_seed(4)
+    c = Pair(2, 2, 1, 16, 32, I8, I8)
+    k = rows(gen, 80, 1, 32, torch.float16)
+    whole = {x: c.gpu[x].view(torch.uint8).clone() for x in c.gpu}
+    table = c.table.clone()
+    table[1, 0], table[1, 1] = -7, 1000
+    start = torch.tensor([0, 40, 80], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([-3, 0], dtype=torch.int32, device="cuda")
+    B.mnnq_kv_append(k.cuda(), k.cuda(), *c.args()[:4], table.cuda(), lengths, start=start)
+    c.ref.append("k", c.table[0], 0, k[:32])
+    c.ref.append("v", c.table[0], 0, k[:32])
+    c.lengths = [32, 0]
+    c.check()
+    others = [i for i in range(c.gpu["k_codes"].shape[0]) if i not in c.table[0].tolist()]
+    for x in ("k_codes", "v_codes"):
+        assert torch.equal(c.gpu[x].view(torch.uint8)[others], whole[x][others])
+
+
+def test_not_a_number_stays_in_its_block():
+    gen = torch.Generator().manual_seed(5)
+    c = Pair(1, 4, 2, 16, 32, I8, F8)
+    k, v = rows(gen, 64, 2, 32, torch.float16), rows(gen, 64, 2, 32, torch.float16)
+    k[20, 1, 3], v[40, 0, 0] = float("nan"), float("inf")
+    B.mnnq_kv_append(k.cuda(), v.cuda(), *c.args())
+    k[20, 1, 3], v[40, 0, 0] = 0, 0
+    c.ref.append("k", c.table[0], 0, k)
+    c.ref.append("v", c.table[0], 0, v)
+    for x, (b, h) in (("k", (1, 1)), ("v", (2, 0))):
+        at = int(c.table[0, b])
+        r = c.gpu[x + "_range"].cpu()
+        assert not torch.isfinite(r[at, h])
+        codes = c.gpu[x + "_codes"].view(torch.uint8).cpu().view(c.ref.type[x]).double()
+        for i in range(4):
+            for j in range(2):
+                if (i, j) != (b, h):
+                    place = int(c.table[0, i])
+                    assert float(r[place, j]) == float(c.ref.range[x][place, j])
+                    assert torch.equal(codes[place, j], c.ref.codes[x][place, j])
+
+
+# ---- evict
+
+def sums(gen, shape):
+    w = torch.exp(2 * torch.randn(shape, generator=gen))
+    few = torch.rand(shape, generator=gen)
+    return torch.where(few < 0.2, torch.zeros(()), torch.where(few < 0.5, torch.full((), 0.25), w))
+
+
+def run_evict(c, w, keep, recent, new_table, stride):
+    nw = torch.full((w.shape[0], w.shape[1], stride), 9.0, device="cuda")
+    kept, left = B.mnnq_kv_evict(*c.args(), w.cuda(), keep, recent, new_table.cuda(), nw)
+    want = R.evict(c.ref, c.table, c.lengths, w, keep, recent, new_table)
+    lens = [min(n, keep) for n in c.lengths]
+    assert left.tolist() == lens
+    for (s, h), places in want.items():
+        assert kept[s, h].tolist() == places + [-1] * (keep - len(places)), (s, h)
+        assert torch.equal(nw[s, h, :len(places)].cpu(), w[s, h][torch.tensor(places, dtype=torch.long)])
+        assert not nw[s, h, len(places):].any()
+    c.check(new_table, lens)
+
+
+@pytest.mark.parametrize("k_type,v_type,dim,block", [(I8, I8, 128, 64), (F8, F8, 64, 16), (I8, F8, 80, 32), (F8, I8, 256, 128)])
+@pytest.mark.parametrize("keep,recent", [(1, 0), (1, 1), (40, 8), (64, 64), (129, 0), (400, 100)])
+def test_evict(k_type, v_type, dim, block, keep, recent):
+    gen = torch.Generator().manual_seed(keep)
+    lengths = [300, 1, 64, 0, 401]
+    print("evict", k_type, v_type, dim, block, keep, recent, flush=True)
+    per = -(-max(lengths) // block)
+    more = -(-keep // block)
+    c = Pair(5, per, 2, block, dim, k_type, v_type, spare=5 * more)
+    k, v = rows(gen, sum(lengths), 2, dim, torch.float16), rows(gen, sum(lengths), 2, dim, torch.float16)
+    c.append(k, v, lengths)
+    run_evict(c, sums(gen, (5, 2, per * block)), keep, recent, c.free.view(5, more), keep + 3)
+
+
+def test_evict_extremes_of_the_weights():
+    """All the same, zeros of both signs, infinities, negative numbers; NaN is above everything."""
+    gen = torch.Generator().manual_seed(2)
+    c = Pair(1, 8, 6, 16, 16, I8, I8, spare=3)
+    k = rows(gen, 128, 6, 16, torch.float16)
+    c.append(k, k, [128])
+    w = torch.zeros(1, 6, 128)
+    w[0, 0] = 0.5
+    w[0, 1, ::2] = -0.0
+    w[0, 2] = torch.randn(128, generator=gen)
+    w[0, 3, 100:] = float("inf")
+    w[0, 4, 5] = float("-inf")
+    w[0, 4, 50:60] = 1e-42                      # subnormal numbers are numbers
+    run_evict(c, w, 40, 4, c.free.view(1, 3), 48)
+    w[0, 5, 7] = float("nan")
+    nw = torch.empty((1, 6, 40), device="cuda")
+    kept, _ = B.mnnq_kv_evict(*c.args(), w.cuda(), 40, 4, c.free.view(1, 3).cuda(), nw)
+    assert kept[0, 5].tolist() == [*range(35), *range(124, 128), -1][:39] + [127] or 7 in kept[0, 5].tolist()
+
+
+def test_evict_many_tokens():
+    gen = torch.Generator().manual_seed(6)
+    c = Pair(1, 80, 1, 128, 16, I8, F8, spare=32)
+    k = rows(gen, 10000, 1, 16, torch.float16)
+    c.append(k, k, [10000])
+    run_evict(c, sums(gen, (1, 1, 10000)), 4000, 100, c.free.view(1, 32), 4096)
+
+
+def test_evict_room_of_the_new_table():
+    """The kept tokens are cut to the room that the new table has."""
+    gen = torch.Generator().manual_seed(7)
+    c = Pair(1, 4, 1, 16, 16, I8, I8, spare=2)
+    k = rows(gen, 60, 1, 16, torch.float16)
+    c.append(k, k, [60])
+    w = sums(gen, (1, 1, 64))
+    nw = torch.empty((1, 1, 50), device="cuda")
+    kept, left = B.mnnq_kv_evict(*c.args(), w.cuda(), 50, 10, c.free.view(1, 2).cuda(), nw)
+    want = R.evict(c.ref, c.table, [60], w, 32, 10, c.free.view(1, 2))[0, 0]
+    assert left.tolist() == [32] and kept[0, 0].tolist() == want + [-1] * 18
