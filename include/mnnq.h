@@ -339,7 +339,7 @@ typedef enum { MNNQ_KV_INT8 = 0, MNNQ_KV_FP8 = 1 } mnnq_kv_form;
 /* A cache, and the sequences in it.  A HOST structure of device pointers; calls read it before they return.
  * Token t of sequence s is token t % block_tokens of block block_table[s * table_blocks + t / block_tokens];
  * blocks are the caller's to give out, no two sequences may append to the same one.  Entries of the table
- * behind a sequence's last token are not read. */
+ * behind a sequence's last token may hold anything. */
 typedef struct {
     void *k_codes, *v_codes;        /* [blocks, kv_heads, block_tokens, head_dim], one byte each, 16-byte aligned */
     float *k_range, *v_range;       /* [blocks, kv_heads] */

@@ -91,6 +91,24 @@ __device__ __forceinline__ half8v codes_to_half8(uint32_t w0, uint32_t w1)
     return half8v{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
+// Byte b (0..3) of four dwords as exact halves.
+template <int FORM>
+__device__ __forceinline__ void byte_to_half(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, int b, half2v& lo, half2v& hi)
+{
+    if (FORM == MNNQ_KV_FP8) {
+        const uint32_t pair = (uint32_t)(0x0c0c0000 | (4 + b) << 8 | b);
+        const uint32_t w = __builtin_amdgcn_perm(w1, w0, pair), v = __builtin_amdgcn_perm(w3, w2, pair);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, false);
+    } else {
+        // (a byte c under a byte of zeros, with the bits of 0x6480 turned over, is the half 1024 + 128 + c)
+        const uint32_t pair = (uint32_t)(0x0c000c00 | (4 + b) << 16 | b);
+        const half2v mid = {(_Float16)1152.0f, (_Float16)1152.0f};
+        lo = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(w1, w0, pair) ^ 0x64806480u) - mid;
+        hi = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(w3, w2, pair) ^ 0x64806480u) - mid;
+    }
+}
+
 // The four codes of a dword as numbers, exact.
 template <int FORM>
 __device__ __forceinline__ void codes_to_float(uint32_t w, float (&v)[4])

@@ -9,6 +9,7 @@ namespace {
 
 constexpr int64_t kMaxGridYZ = 65535;
 constexpr int64_t kMaxRows = (int64_t)1 << 31;           // tokens are indexed by int32 arrays
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence in a cache
 constexpr int64_t kMaxStride = (int64_t)1 << 23;         // 64 rows within 32-bit byte offsets
 
 inline bool misaligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
@@ -45,7 +46,7 @@ int check_cache(const mnnq_kv_cache* c)
         return MNNQ_ERR_UNSUPPORTED;
     if ((c->k_form != MNNQ_KV_INT8 && c->k_form != MNNQ_KV_FP8) || (c->v_form != MNNQ_KV_INT8 && c->v_form != MNNQ_KV_FP8))
         return MNNQ_ERR_UNSUPPORTED;
-    if (c->blocks > kMaxRows || c->sequences > kMaxGridYZ || c->table_blocks > kMaxRows / c->block_tokens)
+    if (c->blocks > kMaxRows || c->sequences > kMaxGridYZ || c->table_blocks > kMaxTokens / c->block_tokens)
         return MNNQ_ERR_UNSUPPORTED;
     if (misaligned(c->k_codes, 16) || misaligned(c->v_codes, 16) || misaligned(c->k_range, 4) || misaligned(c->v_range, 4) ||
         misaligned(c->block_table, 4) || misaligned(c->lengths, 4))
@@ -154,7 +155,7 @@ int mnnq_kv_evict(const mnnq_kv_cache* cache, const float* weights, int64_t weig
     if (!weights || !new_table || !kept || !new_lengths || !new_weights) return MNNQ_ERR_NULL;
     if (keep <= 0 || recent < 0 || recent > keep || weights_stride <= 0 || new_table_blocks <= 0) return MNNQ_ERR_SHAPE;
     if (new_weights_stride < keep) return MNNQ_ERR_SIZE;
-    if (keep >= kMaxRows || new_table_blocks >= kMaxRows / cache->block_tokens || 2 * cache->kv_heads > kMaxGridYZ)
+    if (keep > kMaxTokens || new_table_blocks > kMaxTokens / cache->block_tokens || 2 * cache->kv_heads > kMaxGridYZ)
         return MNNQ_ERR_UNSUPPORTED;
     if (misaligned(weights, 4) || misaligned(new_table, 4) || misaligned(kept, 4) || misaligned(new_lengths, 4) ||
         misaligned(new_weights, 4))

@@ -4,14 +4,15 @@
 // time: S = K Q^T with tokens down and rows across (v_mfma_f32_16x16x32_f16), O^T = V^T P^T.  Tokens-down puts a row's scores
 // into the lanes of one column, where the next product wants its probabilities: the four scores of a lane in two tiles of 16
 // tokens are its eight values of P^T as they stand.
-//   * Codes become halves exactly; queries become halves scaled by a power of two per row so that the greatest is in
-//     [2^14, 2^15) - exact down to 2^-39 of it for bfloat16 too - and ranges, scale and that power are one factor per row and
-//     block applied to the fp32 sums.
+//   * Codes become halves exactly; bfloat16 queries become halves scaled by a power of two per row so that the greatest is in
+//     [2^14, 2^15), exact down to 2^-39 of it; ranges, scale and that power are one factor per row and block applied to the
+//     fp32 sums.
 //   * V's range goes into P: p r / U, U the greatest range so far (the accumulators are rescaled when it grows).  Probabilities
-//     are kept under 2^14 instead of 1 so that a half holds them down to 2^-38.
-// A wave takes 32 tokens at a time, with the codes of its next 32 in flight; four waves of a workgroup share a part of the
+//     stay below 2^14 instead of 1, so that a half holds them down to 2^-32 of the greatest.
+// A wave takes 32 tokens at a time, with the codes of its next 32 in flight; the waves of a workgroup share a part of the
 // sequence and join through LDS, the parts are joined by a second kernel.
 #include "mnnq_attn.h"
+#include "mnnq_forms.h"
 
 namespace mnnq {
 
@@ -19,34 +20,79 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kStep = 32;                        // tokens of a wave's step
-constexpr float kTopBits = 13.0f;                // probabilities are p 2^13 where the running maximum is the row's
+constexpr float kTopBits = 8.0f;                 // a probability at the running maximum is 2^8
+constexpr float kSlack = 6.0f;                   // the running maximum follows when it is 2^6 behind
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -3.402823466e38f;
+constexpr float kLeastNormal = 1.17549435e-38f;
+constexpr int kOutOfRange = 0x7ffffff0;          // a byte offset beyond every piece: loads give 0
 
 struct DecodeArgs {
     mnnq_kv_cache c;
     Rows q, out;
-    float* part;                                 // partial results, NULL with one part
-    float* scores;                               // [sequences, heads, tokens, bound] where weights are asked for
-    int64_t tokens, bound, part_len, parts;
-    int heads, group, rows;                      // rows: group * tokens
+    float* sums;                                 // [sequences, kv_heads, rows, parts, DP] where there is more than one part
+    float2* stats;                               // [sequences, kv_heads, rows, parts]: maximum (log2) and sum
+    float* scores;                               // [sequences, kv_heads, rows, scores_stride] where weights are asked for
+    float* weights;
+    int64_t tokens, scores_stride, weights_stride;
+    int bound, part_len, parts;
+    int group, rows;                             // rows: group * tokens
     float scale_log2;
     bool bf16;
 };
 
-// Partial result of a part and row: DP sums, then the maximum and the sum of the probabilities.
-__host__ __device__ inline int64_t part_floats(int DP) { return DP + 2; }
+__device__ __forceinline__ int length_of(const DecodeArgs& a, int64_t s)
+{
+    const int n = a.c.lengths[s];
+    return n < 0 ? 0 : n > a.bound ? a.bound : n;
+}
+
+// Maximum over the four lanes of a column (l, l + 16, l + 32, l + 48), the same in all of them.
+__device__ __forceinline__ float column_max(float v)
+{
+    const u2v a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const u2v b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// N 16-byte pieces of a bfloat16 query row per lane as halves times 2^up, up such that the row's greatest is in [2^14, 2^15).
+template <int N>
+__device__ __forceinline__ int scale_query(const u4v (&raw)[N], half8v (&out)[N])
+{
+    typedef unsigned short us2v __attribute__((ext_vector_type(2)));
+    us2v two = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) two = __builtin_elementwise_max(two, __builtin_bit_cast(us2v, raw[i][j] & 0x7fff7fffu));
+    uint32_t top = max((uint32_t)two.x, (uint32_t)two.y);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    const int up = max(-126, min(126, 14 + 127 - (int)(top >> 7)));      // (the exponent's bits)
+    const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const half2v h = __builtin_bit_cast(half2v, pack16(__uint_as_float(raw[i][j] << 16) * mul,
+                                                               __uint_as_float(raw[i][j] & 0xffff0000u) * mul, false));
+            out[i][2 * j] = h.x, out[i][2 * j + 1] = h.y;
+        }
+    return up;
+}
 
 template <int DP, int KF, int VF, int MT>
-__global__ __launch_bounds__(64 * kWaves) void decode_kernel(DecodeArgs a, const int32_t* __restrict__ tables,
-                                                               const float* __restrict__ k_ranges,
-                                                               const float* __restrict__ v_ranges)
+__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(DecodeArgs a, const int32_t* __restrict__ tables,
+                                                              const float* __restrict__ k_ranges,
+                                                              const float* __restrict__ v_ranges)
 {
     constexpr int KC = DP / 64;                  // 16-byte pieces of a K row per lane
     constexpr int VB = DP / 16;                  // bytes of a V row per lane
     constexpr int VW = VB / 4;
     constexpr int ND = DP / 16;                  // matrix instructions of O^T per row tile
-    constexpr int DH = DP < 128 ? DP : 128;      // values of a row that the waves join at a time
+    constexpr int DH = DP < 512 / kWaves ? DP : 512 / kWaves;      // values of a row that the waves join at a time
+    constexpr int kStride = kWaves * kStep;
     __shared__ __align__(16) float red[kWaves][16 * (DH + 4)];
     __shared__ float red_m[kWaves][16], red_l[kWaves][16];
 
@@ -56,57 +102,111 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(DecodeArgs a, const
     const int D = c.head_dim, B = c.block_tokens;
     const int64_t s = blockIdx.z;
     const int kvh = blockIdx.y % c.kv_heads, row0 = (blockIdx.y / c.kv_heads) * 16 * MT;
-    int64_t len = c.lengths[s];
-    len = len < 0 ? 0 : len > a.bound ? a.bound : len;
-    const int64_t p0 = blockIdx.x * a.part_len;
-    if (p0 >= len && !(p0 == 0 && a.parts == 1)) return;        // (one part: rows of zeros are stored)
-    const int64_t p1 = p0 + a.part_len < len ? p0 + a.part_len : len;
-    const int32_t* table = tables + s * c.table_blocks;
     const int block_shift = __builtin_ctz(B);
+    const int p0 = blockIdx.x * a.part_len;
+    int p = p0 + wave * kStep;
+
+    // Entries of the table are fetched two steps ahead, the length beside the first ones (an entry behind the last token is
+    // of no use, and does no harm).
+    const int32_t* table = tables + s * c.table_blocks;
+    const int last_entry = (int)c.table_blocks - 1;
+    struct Entries {
+        int at[2];
+    };
+    auto find = [&](int p) {
+        const int n = p >> block_shift, m = (p + 16) >> block_shift;
+        return Entries{{table[n < last_entry ? n : last_entry], table[m < last_entry ? m : last_entry]}};
+    };
+    Entries ahead = find(p);
+    const int len = length_of(a, s);
+    if (p0 >= len && a.parts > 1) return;        // (one part: rows of zeros are stored)
+    const int p1 = p0 + a.part_len < len ? p0 + a.part_len : len;
+
+    // The codes of a step: two tiles of 16 tokens; there: 0 where the cache has no such block.
+    struct Codes {
+        bool there[2];
+        u4v k[2][KC];
+        uint32_t v[8][VW];
+        float kr[2], vr[2];
+    };
+    int k_off[KC], v_off[4];
+#pragma unroll
+    for (int j = 0; j < KC; ++j) k_off[j] = 64 * j + 16 * g < D ? col * D + 16 * g + 64 * j : kOutOfRange;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v_off[j] = VB * col < D ? (4 * g + j) * D + VB * col : kOutOfRange;
+    auto load = [&](int p, const Entries& b, Codes& x) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = p + 16 * i;
+            x.there[i] = (uint32_t)b.at[i] < (uint32_t)c.blocks;
+            const int64_t slot = (int64_t)(x.there[i] ? b.at[i] : 0) * c.kv_heads + kvh;
+            // (rows behind the last token may hold anything, NaN codes among it: they are beyond the piece and come as zeros)
+            const int left = p1 - at < 16 ? p1 - at : 16;
+            const int bytes = x.there[i] && left > 0 ? left * D : 0;
+            const int64_t from = (slot * B + (at & (B - 1))) * D;
+            const __amdgpu_buffer_rsrc_t rk = rsrc(static_cast<const uint8_t*>(c.k_codes) + from, bytes);
+            const __amdgpu_buffer_rsrc_t rv = rsrc(static_cast<const uint8_t*>(c.v_codes) + from, bytes);
+#pragma unroll
+            for (int j = 0; j < KC; ++j) x.k[i][j] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off[j], 0, 0));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (VW == 1) {
+                    x.v[4 * i + j][0] = __builtin_amdgcn_raw_buffer_load_b32(rv, v_off[j], 0, 0);
+                } else if constexpr (VW == 2) {
+                    const u2v w = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(rv, v_off[j], 0, 0));
+                    x.v[4 * i + j][0] = w.x, x.v[4 * i + j][1] = w.y;
+                } else {
+                    const u4v w = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(rv, v_off[j], 0, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x.v[4 * i + j][e] = w[e];
+                }
+            }
+            x.kr[i] = k_ranges[slot];
+            x.vr[i] = v_ranges[slot];
+        }
+    };
+    // What the scalar loads of the step before brought is taken before new ones are requested: they return in any order, so that
+    // a wait for one is a wait for all.
+    auto arrived = [&](Codes& x, Entries& b) {
+        asm volatile("" : "+s"(x.kr[0]), "+s"(x.kr[1]), "+s"(x.vr[0]), "+s"(x.vr[1]), "+s"(b.at[0]), "+s"(b.at[1]));
+    };
+
+    Codes x0, x1;
+    if (p < p1) load(p, ahead, x0);
+    ahead = find(p + kStride);
 
     // queries, their power of two, and how far each row sees
     half8v qf[MT][2 * KC];
     float factor[MT];
-    int64_t limit[MT];
-    int64_t lowest_limit = len;
+    int limit[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int r = row0 + m * 16 + col;
         const bool there = r < a.rows;
         const int t = there ? r / a.group : 0;
         const int h = kvh * a.group + (there ? r - t * a.group : 0);
-        limit[m] = there ? len - a.tokens + t + 1 : 0;
+        limit[m] = there ? len - (int)a.tokens + t + 1 : 0;
         const uint16_t* src = a.q.data + (s * a.tokens + t) * a.q.token + h * a.q.head;
         u4v raw[2 * KC];
-        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 2 * KC; ++i) {
             const int d = 64 * (i / 2) + 16 * g + 8 * (i & 1);
-            raw[i] = there && d < D ? *reinterpret_cast<const u4v*>(src + d) : u4v{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = max(top, max(raw[i][j] & 0x7fffu, (raw[i][j] >> 16) & 0x7fffu));
+            raw[i] = u4v{0, 0, 0, 0};
+            if (there && d < D) raw[i] = *reinterpret_cast<const u4v*>(src + d);
         }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        // exponent e with 2^e <= greatest < 2^(e+1)
-        const int e = (int)(__float_as_uint(value16(top, a.bf16)) >> 23) - 127;
-        const int up = max(-126, min(126, 14 - e));
-        const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-        factor[m] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+        factor[m] = a.scale_log2;
+        if (a.bf16) {
+            factor[m] *= __uint_as_float((uint32_t)(127 - scale_query(raw, qf[m])) << 23);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2 * KC; ++i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                qf[m][i][2 * j] = (_Float16)(value16(raw[i][j] & 0xffffu, a.bf16) * mul);
-                qf[m][i][2 * j + 1] = (_Float16)(value16(raw[i][j] >> 16, a.bf16) * mul);
-            }
+            for (int i = 0; i < 2 * KC; ++i) qf[m][i] = __builtin_bit_cast(half8v, raw[i]);
         }
     }
-    lowest_limit = len - a.tokens + 1;           // tokens below it are seen by every row
+    const int lowest_limit = len - (int)a.tokens + 1;             // tokens below it are seen by every row
 
     f4v o[MT][ND];
     float mx[MT], l[MT];
-    float unit = 0.0f;                           // U
+    float unit = 0.0f, inv_unit = 0.0f;          // U and 1 / U
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         mx[m] = kLowest;
@@ -115,61 +215,7 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(DecodeArgs a, const
         for (int i = 0; i < ND; ++i) o[m][i] = f4v{0, 0, 0, 0};
     }
 
-    struct Codes {
-        u4v k[2][KC];
-        uint32_t v[8][VW];
-        int64_t block[2];
-    };
-    // block of the 16 tokens from p on; -1: none of ours
-    auto block_at = [&](int64_t p) -> int64_t {
-        if (p >= p1) return -1;
-        const int64_t b = __builtin_amdgcn_readfirstlane(table[p >> block_shift]);
-        return b >= 0 && b < c.blocks ? b : -1;
-    };
-    auto load = [&](int64_t p, Codes& x) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t at = p + 16 * i;
-            x.block[i] = block_at(at);
-            const int64_t block = x.block[i] < 0 ? 0 : x.block[i];
-            const int64_t base = ((block * c.kv_heads + kvh) * B + (at & (B - 1))) * D;
-            const uint8_t* kp = static_cast<const uint8_t*>(c.k_codes) + base + col * D + 16 * g;
-            const uint8_t* vp = static_cast<const uint8_t*>(c.v_codes) + base + 4 * g * D + VB * col;
-#pragma unroll
-            for (int j = 0; j < KC; ++j)
-                x.k[i][j] = x.block[i] >= 0 && 64 * j + 16 * g < D ? *reinterpret_cast<const u4v*>(kp + 64 * j)
-                                                                   : u4v{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool in = x.block[i] >= 0 && VB * col < D;
-                if (VW == 1) {
-                    x.v[4 * i + j][0] = in ? *reinterpret_cast<const uint32_t*>(vp + j * D) : 0;
-                } else if (VW == 2) {
-                    const u2v w = in ? *reinterpret_cast<const u2v*>(vp + j * D) : u2v{0, 0};
-                    x.v[4 * i + j][0] = w.x, x.v[4 * i + j][1 % VW] = w.y;
-                } else {
-                    const u4v w = in ? *reinterpret_cast<const u4v*>(vp + j * D) : u4v{0, 0, 0, 0};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x.v[4 * i + j][e % VW] = w[e];
-                }
-            }
-        }
-    };
-
-    Codes next;
-    int64_t p = p0 + wave * kStep;
-    if (p < p1) load(p, next);
-    for (; p < p1; p += kWaves * kStep) {
-        Codes x = next;
-        if (p + kWaves * kStep < p1) load(p + kWaves * kStep, next);
-        float kr[2], vr[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t at = (x.block[i] < 0 ? 0 : x.block[i]) * c.kv_heads + kvh;
-            kr[i] = x.block[i] < 0 ? 0.0f : k_ranges[at] * (1.0f / code_top<KF>());
-            vr[i] = x.block[i] < 0 ? 0.0f : v_ranges[at];
-        }
-        // scores
+    auto step = [&](int p, const Codes& x) {
         f4v sc[MT][2];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -187,121 +233,125 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(DecodeArgs a, const
                     sc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[m][2 * j + 1], sc[m][i], 0, 0, 0);
                 }
             }
-        const bool masked = p + kStep > lowest_limit || p + kStep > p1 || x.block[0] < 0 || x.block[1] < 0;
+        const bool masked = p + kStep > lowest_limit || p + kStep > p1 || !x.there[0] || !x.there[1];
         // (a range that is not finite is that of undefined values, which only rows that see them may get)
-        const float vmax = fmaxf(vr[0] < __builtin_inff() ? vr[0] : 0.0f, vr[1] < __builtin_inff() ? vr[1] : 0.0f);
+        const float v0 = x.there[0] ? x.vr[0] : 0.0f, v1 = x.there[1] ? x.vr[1] : 0.0f;
+        const float vmax = fmaxf(v0 < __builtin_inff() ? v0 : 0.0f, v1 < __builtin_inff() ? v1 : 0.0f);
+        float less_unit = 1.0f;                  // what the accumulators take of U's growth
         if (vmax > unit) {
-            const float down = unit / fmaxf(vmax, 1.17549435e-38f);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < ND; ++i) o[m][i] *= down;
-            unit = fmaxf(vmax, 1.17549435e-38f);
+            const float now = fmaxf(vmax, kLeastNormal);
+            less_unit = unit / now;
+            unit = now;
+            inv_unit = 1.0f / now;
         }
-        const float inv_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
+        const float ratio[2] = {v0 * inv_unit, v1 * inv_unit};
         half8v pf[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+            uint32_t hidden = 0;
+            if (masked)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = p + 16 * (i / 4) + 4 * g + (i & 3);
+                    if (t >= limit[m] || t >= p1 || !x.there[i / 4]) {
+                        hidden |= 1u << i;
+                        sc[m][i / 4][i & 3] = -__builtin_inff();
+                    }
+                }
+            // (the factor is positive, or 0 or NaN with a range that is)
+            const float f[2] = {factor[m] * (x.kr[0] * (1.0f / code_top<KF>())), factor[m] * (x.kr[1] * (1.0f / code_top<KF>()))};
             float top = kLowest;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float f = factor[m] * kr[i];
+            for (int i = 0; i < 2; ++i)
+                top = fmaxf(top, f[i] * fmaxf(fmaxf(sc[m][i][0], sc[m][i][1]), fmaxf(sc[m][i][2], sc[m][i][3])));
+            if (a.scores && row0 + m * 16 + col < a.rows) {
+                float* to = a.scores + ((s * c.kv_heads + kvh) * a.rows + row0 + m * 16 + col) * a.scores_stride + p + 4 * g;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sc[m][i][e] *= f;
-                    if (masked) {
-                        const int64_t t = p + 16 * i + 4 * g + e;
-                        if (t >= limit[m] || t >= p1 || x.block[i] < 0) sc[m][i][e] = -__builtin_inff();
-                    }
-                    top = fmaxf(top, sc[m][i][e]);
+                for (int i = 0; i < 2; ++i) {
+                    f4v z = sc[m][i] * f[i];
+                    if (masked)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (hidden >> (4 * i + e) & 1) z[e] = -__builtin_inff();
+                    *reinterpret_cast<f4v*>(to + 16 * i) = z;
                 }
             }
-            if (a.scores && row0 + m * 16 + col < a.rows) {
-                const int r = row0 + m * 16 + col;
-                float* to = a.scores + ((s * c.kv_heads + kvh) * a.rows + r) * a.bound;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t t = p + 16 * i + 4 * g + e;
-                        if (t < p1) to[t] = sc[m][i][e];
-                    }
-            }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(mx[m], top);
-            if (__ballot(now > mx[m])) {
+            top = column_max(top);
+            const bool follow = __ballot(top > mx[m] + kSlack) != 0;
+            if (follow || less_unit != 1.0f) {
+                const float now = follow ? fmaxf(mx[m], top) : mx[m];
                 const float down = __builtin_amdgcn_exp2f(mx[m] - now);
                 mx[m] = now;
                 l[m] *= down;
 #pragma unroll
-                for (int i = 0; i < ND; ++i) o[m][i] *= down;
+                for (int i = 0; i < ND; ++i) o[m][i] *= down * less_unit;
             }
+            const float less = kTopBits - mx[m];
             float pr[8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[m][i / 4][i & 3], f[i / 4], less));
+            if (masked)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    pr[4 * i + e] = __builtin_amdgcn_exp2f(sc[m][i][e] - mx[m] + kTopBits);
-                    l[m] += pr[4 * i + e];
-                    pr[4 * i + e] *= vr[i] * inv_unit;
-                    if (masked && sc[m][i][e] == -__builtin_inff()) pr[4 * i + e] = 0.0f;
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (hidden >> i & 1) pr[i] = 0.0f;
+            l[m] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pr[i] *= ratio[i / 4];
+            if (masked)                              // (a ratio that is no number is not theirs)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (hidden >> i & 1) pr[i] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t two = pack16(pr[2 * e], pr[2 * e + 1], false);
-                const half2v h = __builtin_bit_cast(half2v, two);
+                const half2v h = __builtin_bit_cast(half2v, pack16(pr[2 * e], pr[2 * e + 1], false));
                 pf[m][2 * e] = h.x, pf[m][2 * e + 1] = h.y;
             }
         }
-        // what lies behind the last token may be anything, NaN codes among it
-        if (p + kStep > p1) {
+        // V: a byte of four tokens each, twice
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (p + 16 * (j / 4) + 4 * g + (j & 3) >= p1)
-#pragma unroll
-                    for (int e = 0; e < VW; ++e) x.v[j][e] = 0;
-        }
-        // V: bytes of four tokens of a lane turned to four tokens of a byte
-#pragma unroll
-        for (int w = 0; w < VW; ++w) {
-            uint32_t t[2][4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t a0 = x.v[4 * i][w], a1 = x.v[4 * i + 1][w], a2 = x.v[4 * i + 2][w], a3 = x.v[4 * i + 3][w];
-                const uint32_t l01 = __builtin_amdgcn_perm(a1, a0, 0x05010400u), h01 = __builtin_amdgcn_perm(a1, a0, 0x07030602u);
-                const uint32_t l23 = __builtin_amdgcn_perm(a3, a2, 0x05010400u), h23 = __builtin_amdgcn_perm(a3, a2, 0x07030602u);
-                t[i][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
-                t[i][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
-                t[i][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
-                t[i][3] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
-            }
+        for (int w = 0; w < VW; ++w)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const half8v vf = codes_to_half8<VF>(t[0][b], t[1][b]);
+                half8v vf;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    half2v lo, hi;
+                    byte_to_half<VF>(x.v[4 * i][w], x.v[4 * i + 1][w], x.v[4 * i + 2][w], x.v[4 * i + 3][w], b, lo, hi);
+                    vf[4 * i] = lo.x, vf[4 * i + 1] = lo.y, vf[4 * i + 2] = hi.x, vf[4 * i + 3] = hi.y;
+                }
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     o[m][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[m], o[m][4 * w + b], 0, 0, 0);
             }
-        }
+    };
+
+    for (; p < p1; p += 2 * kStride) {
+        const int q = p + kStride;
+        arrived(x0, ahead);
+        if (q < p1) load(q, ahead, x1);
+        ahead = find(q + kStride);
+        step(p, x0);
+        if (q >= p1) break;
+        arrived(x1, ahead);
+        if (q + kStride < p1) load(q + kStride, ahead, x0);
+        ahead = find(q + 2 * kStride);
+        step(q, x1);
     }
 
     // Join the waves: lane (g, col) holds of row col the values d = VB (4 g + v) + i, v = 0..3.
+    const int row = threadIdx.x / (4 * kWaves), at = threadIdx.x % (4 * kWaves);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         float sum = l[m];
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (m > 0) __syncthreads();
-        if (g == 0) red_m[wave][col] = mx[m];
-        if (g == 0) red_l[wave][col] = sum;
+        if (g == 0) red_m[wave][col] = mx[m], red_l[wave][col] = sum;
         __syncthreads();
         float top = red_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][col]);
         const float f = __builtin_amdgcn_exp2f(mx[m] - top) * unit * (1.0f / code_top<VF>());
-        // thread: row tid / 16, DH / 16 values at a time
-        const int row = threadIdx.x >> 4;
         const int r = row0 + m * 16 + row;
         float rt = red_m[0][row];
 #pragma unroll
@@ -310,115 +360,153 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(DecodeArgs a, const
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) rl += red_l[w][row] * __builtin_amdgcn_exp2f(red_m[w][row] - rt);
         const float inv = rl > 0.0f || rl != rl ? 1.0f / rl : 0.0f;
-        const int64_t stat = ((s * c.kv_heads + kvh) * a.rows + r) * a.parts + blockIdx.x;
+        const int64_t part = ((s * c.kv_heads + kvh) * a.rows + r) * a.parts + blockIdx.x;
         const int t = r / a.group, h = kvh * a.group + r - t * a.group;
-        if (a.part && r < a.rows && (threadIdx.x & 15) == 0) {
-            a.part[stat * part_floats(DP) + DP] = rt;
-            a.part[stat * part_floats(DP) + DP + 1] = rl;
-        }
+        if (a.stats && r < a.rows && at == 0) a.stats[part] = float2{rt, rl};
 #pragma unroll
         for (int first = 0; first < DP; first += DH) {
             if (first > 0) __syncthreads();
-            if (DP == DH || (4 * g * VB) / DH == first / DH)
+            // (a row's pieces of 4 VB values: in one half or quarter each)
+            if (4 * g * VB / DH == first / DH)
 #pragma unroll
                 for (int i = 0; i < ND; ++i)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) red[wave][col * (DH + 4) + VB * (4 * g + v) + i - first] = o[m][i][v] * f;
             __syncthreads();
-            const int d0 = (threadIdx.x & 15) * (DH / 16);
-            float val[DH / 16];
+            constexpr int N = DH / (4 * kWaves);
+            const int d = first + at * N;
+            float val[N];
 #pragma unroll
-            for (int i = 0; i < DH / 16; ++i) {
+            for (int i = 0; i < N; ++i) {
                 val[i] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) val[i] += red[w][row * (DH + 4) + d0 + i];
+                for (int w = 0; w < kWaves; ++w) val[i] += red[w][row * (DH + 4) + at * N + i];
             }
-            if (r >= a.rows) continue;
-            // (head_dim is a multiple of 16, so of the values of a thread)
-            if (first + d0 < D) {
-                if (a.parts > 1) {
-                    float* to = a.part + stat * part_floats(DP) + first + d0;
+            if (r >= a.rows || d >= D) continue;     // (head_dim is a multiple of a thread's values)
+            if (a.parts > 1) {
+                float* to = a.sums + part * DP + d;
 #pragma unroll
-                    for (int i = 0; i < DH / 16; ++i) to[i] = val[i];
-                } else {
-                    uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head + first + d0;
+                for (int i = 0; i < N; ++i) to[i] = val[i];
+            } else {
+                uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head + d;
 #pragma unroll
-                    for (int i = 0; i < DH / 16; i += 2)
-                        *reinterpret_cast<uint32_t*>(to + i) = pack16(val[i] * inv, val[i + 1] * inv, a.bf16);
-                }
+                for (int i = 0; i < N; i += 2)
+                    *reinterpret_cast<uint32_t*>(to + i) = pack16(val[i] * inv, val[i + 1] * inv, a.bf16);
             }
         }
     }
 }
 
-// Joins the parts of a row: one workgroup per row, a thread per two values and every fourth... of the parts.
+constexpr int kJoinThreads = 256;
+constexpr int kMaxParts = 1024;
+constexpr int kEarly = 4;                        // sums that a thread of a join requests before it knows the length
+constexpr int kRowsAtOnce = 64;                  // rows whose statistics a workgroup holds
+
+// Behind the parts.  Workgroups below a.rows (where there are several parts): one row's parts joined.  The others: attention
+// given to kJoinThreads tokens.
 template <int DP>
-__global__ __launch_bounds__(256) void join_kernel(DecodeArgs a)
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
 {
-    constexpr int PER = DP / 2;                  // threads of a part: two values each
-    constexpr int TEAMS = 256 / PER;
-    __shared__ float red[TEAMS][DP];
+    constexpr int PER = DP / 4;                  // threads of a part: four values each
+    constexpr int TEAMS = kJoinThreads / PER;
+    __shared__ float f[kMaxParts];
+    __shared__ float wave_top[kJoinThreads / 64], wave_sum[kJoinThreads / 64];
+    __shared__ f4v red[TEAMS][PER];
+    __shared__ float row_top[kRowsAtOnce], row_inv[kRowsAtOnce];
     const mnnq_kv_cache& c = a.c;
-    const int tid = threadIdx.x, team = tid / PER, d = (tid % PER) * 2;
-    const int r = blockIdx.x, kvh = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int kvh = blockIdx.y;
     const int64_t s = blockIdx.z;
-    int64_t len = c.lengths[s];
-    len = len < 0 ? 0 : len > a.bound ? a.bound : len;
-    const int n = (int)((len + a.part_len - 1) / a.part_len);
-    const float* part = a.part + ((s * c.kv_heads + kvh) * a.rows + r) * a.parts * part_floats(DP);
-    float top = kLowest;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, part[i * part_floats(DP) + DP]);
-    float l = 0.0f, v0 = 0.0f, v1 = 0.0f;
-    for (int i = 0; i < n; ++i) {
-        const float* p = part + i * part_floats(DP);
-        const float f = __builtin_amdgcn_exp2f(p[DP] - top);
-        l += p[DP + 1] * f;
-        if (i % TEAMS == team) {
-            v0 += p[d] * f;
-            v1 += p[d + 1] * f;
+    const int joins = a.parts > 1 ? a.rows : 0;
+    if ((int)blockIdx.x < joins) {
+        // The length and the first of the sums are requested together; what lies in parts behind the length is not looked at.
+        const int r = blockIdx.x, team = tid / PER, d = tid % PER;
+        const int64_t first = ((s * c.kv_heads + kvh) * a.rows + r) * a.parts;
+        const f4v* from = reinterpret_cast<const f4v*>(a.sums + first * DP) + d;
+        f4v early[kEarly];
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) {
+            const int part = i * TEAMS + team;
+            early[i] = from[(int64_t)(part < a.parts ? part : 0) * PER];
+        }
+        const float2 mine = a.stats[first + (tid < a.parts ? tid : 0)];
+        const int n = (length_of(a, s) + a.part_len - 1) / a.part_len;
+        float top = tid < n ? mine.x : kLowest;
+        for (int i = tid + kJoinThreads; i < n; i += kJoinThreads) top = fmaxf(top, a.stats[first + i].x);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        if (lane == 0) wave_top[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kJoinThreads / 64; ++w) top = fmaxf(top, wave_top[w]);
+        float l = 0.0f;
+        for (int i = tid; i < n; i += kJoinThreads) {
+            const float2 st = i == tid ? mine : a.stats[first + i];
+            f[i] = __builtin_amdgcn_exp2f(st.x - top);
+            l += st.y * f[i];
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) l += __shfl_xor(l, m);
+        if (lane == 0) wave_sum[wave] = l;
+        __syncthreads();
+        l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kJoinThreads / 64; ++w) l += wave_sum[w];
+        f4v v = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i)
+            if (i * TEAMS + team < n) v += early[i] * f[i * TEAMS + team];
+#pragma unroll 8
+        for (int i = kEarly * TEAMS + team; i < n; i += TEAMS) v += from[(int64_t)i * PER] * f[i];
+        red[team][d] = v;
+        __syncthreads();
+        if (team == 0 && 4 * d < c.head_dim) {
+#pragma unroll
+            for (int i = 1; i < TEAMS; ++i) v += red[i][d];
+            const int t = r / a.group, h = kvh * a.group + r - t * a.group;
+            v *= l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head;
+            *reinterpret_cast<u2v*>(to + 4 * d) = u2v{pack16(v.x, v.y, a.bf16), pack16(v.z, v.w, a.bf16)};
+        }
+        return;
+    }
+    const int len = length_of(a, s), n = (len + a.part_len - 1) / a.part_len;
+    const int64_t t0 = (int64_t)((int)blockIdx.x - joins) * kJoinThreads, t = t0 + tid;
+    if (t0 >= len) return;
+    const int64_t row0 = (s * c.kv_heads + kvh) * a.rows;
+    float sum = 0.0f;
+    for (int base = 0; base < a.rows; base += kRowsAtOnce) {
+        const int rows = a.rows - base < kRowsAtOnce ? a.rows - base : kRowsAtOnce;
+        __syncthreads();
+        for (int r = wave; r < rows; r += kJoinThreads / 64) {
+            const float2* st = a.stats + (row0 + base + r) * a.parts;
+            float top = kLowest, l = 0.0f;
+            for (int i = lane; i < n; i += 64) top = fmaxf(top, st[i].x);
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+            for (int i = lane; i < n; i += 64) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - top);
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) l += __shfl_xor(l, m);
+            // (a row that sees nothing gives nothing)
+            if (lane == 0) row_top[r] = top - kTopBits, row_inv[r] = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        }
+        __syncthreads();
+        if (t < len) {
+            const float* from = a.scores + (row0 + base) * a.scores_stride + t;
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r) sum += __builtin_amdgcn_exp2f(from[r * a.scores_stride] - row_top[r]) * row_inv[r];
         }
     }
-    red[team][d] = v0, red[team][d + 1] = v1;
-    __syncthreads();
-    if (team == 0 && d < c.head_dim) {
-#pragma unroll
-        for (int i = 1; i < TEAMS; ++i) v0 += red[i][d], v1 += red[i][d + 1];
-        const int t = r / a.group, h = kvh * a.group + r - t * a.group;
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head;
-        *reinterpret_cast<uint32_t*>(to + d) = pack16(v0 * inv, v1 * inv, a.bf16);
-    }
-}
-
-// Adds the attention given to every token: a thread per token, the rows' maxima and sums from the scores' parts.
-__global__ __launch_bounds__(256) void weights_kernel(DecodeArgs a, float* weights, int64_t stride, int DP)
-{
-    const mnnq_kv_cache& c = a.c;
-    const int64_t s = blockIdx.z;
-    const int kvh = blockIdx.y;
-    int64_t len = c.lengths[s];
-    len = len < 0 ? 0 : len > a.bound ? a.bound : len;
-    const int64_t t = blockIdx.x * 256 + threadIdx.x;
-    if (blockIdx.x * 256 >= len) return;
-    const int n = (int)((len + a.part_len - 1) / a.part_len);
-    float sum = 0.0f;
-    for (int r = 0; r < a.rows; ++r) {
-        const int64_t row = (s * c.kv_heads + kvh) * a.rows + r;
-        const float* part = a.part + row * a.parts * part_floats(DP);
-        float top = kLowest, l = 0.0f;
-        for (int i = 0; i < n; ++i) top = fmaxf(top, part[i * part_floats(DP) + DP]);
-        for (int i = 0; i < n; ++i) l += part[i * part_floats(DP) + DP + 1] * __builtin_amdgcn_exp2f(part[i * part_floats(DP) + DP] - top);
-        if (t < len && !(l <= 0.0f)) sum += __builtin_amdgcn_exp2f(a.scores[row * a.bound + t] - top + kTopBits) / l;
-    }
-    if (t < len) weights[(s * c.kv_heads + kvh) * stride + t] += sum;
+    if (t < len) a.weights[(s * c.kv_heads + kvh) * a.weights_stride + t] += sum;
 }
 
 struct Plan {
     int DP, MT;
-    int64_t chunks, part_len, parts;
+    int64_t chunks;
+    int part_len, parts;
 };
 
-Plan plan_of(const mnnq_kv_cache& c, int64_t tokens, int heads, int64_t bound, bool weights)
+Plan plan_of(const mnnq_kv_cache& c, int64_t tokens, int heads, int64_t bound)
 {
     Plan p;
     p.DP = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
@@ -426,86 +514,101 @@ Plan plan_of(const mnnq_kv_cache& c, int64_t tokens, int heads, int64_t bound, b
     p.MT = rows > 16 ? 2 : 1;
     p.chunks = (rows + 16 * p.MT - 1) / (16 * p.MT);
     const int64_t base = c.sequences * c.kv_heads * p.chunks;
-    const int64_t want = 2048 / base > 1 ? 2048 / base : 1;
-    int64_t len = (bound + want - 1) / want;
-    len = (len + kWaves * kStep - 1) / (kWaves * kStep) * (kWaves * kStep);
-    p.part_len = len;
-    p.parts = (bound + len - 1) / len;
+    // One sequence: a workgroup per CU, of 128 tokens at least.  Several, of lengths that only the device knows: three per CU, so
+    // that short ones leave no CU idle, of 256 tokens at least (256 wide, where a CU holds one: one).  Measured in us, 256 / 512 / 768
+    // workgroups: 16384 tokens of 8 key heads 13.9 / 14.8 / 14.8, 131072 of 4 33.3 / 33.6 / 34.0; 32 ragged sequences of up to
+    // 6045 61.4 / 53.0 / 49.8; 4 of 8000, 256 wide, 21.4 / 28.3 / 28.4.  Least tokens 128 / 256: 1001 tokens of 4 key heads
+    // 8.4 / 9.5; 8 sequences with weights 19.8 / 18.0.
+    const int64_t most = (c.sequences > 1 && p.DP < 256 ? 768 : 256) / base, least = c.sequences > 1 ? 256 : 128;
+    const int64_t want = most > 0 ? most : 1;
+    int64_t part = (bound + want - 1) / want;
+    if (part < least) part = least;
+    // (up to 512 tokens one part, without the second kernel, is faster: 300 tokens 7.7 against 8.6 us)
+    if (bound <= 512) part = bound;
+    const int64_t whole = kWaves * kStep;
+    part = (part + whole - 1) / whole * whole;
+    if (part * kMaxParts < bound) part = (bound + kMaxParts * whole - 1) / (kMaxParts * whole) * whole;
+    p.part_len = (int)part;
+    p.parts = (int)((bound + part - 1) / part);
     return p;
 }
 
-size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+// Where the workspace's arrays begin, and its size.
+struct Space {
+    size_t stats, scores, total;
+};
 
-size_t part_bytes(const mnnq_kv_cache& c, const Plan& p, int64_t rows, bool weights)
+Space space_of(const mnnq_kv_cache& c, const Plan& p, int64_t rows, int64_t bound, bool weights)
 {
-    if (p.parts == 1 && !weights) return 0;
-    return round16((size_t)(c.sequences * c.kv_heads * rows * p.parts * part_floats(p.DP)) * 4);
+    const auto round16 = [](size_t n) { return (n + 15) / 16 * 16; };
+    const size_t all = (size_t)(c.sequences * c.kv_heads * rows);
+    Space s{0, 0, 0};
+    s.stats = p.parts > 1 ? all * p.parts * p.DP * sizeof(float) : 0;
+    s.scores = s.stats + (p.parts > 1 || weights ? round16(all * p.parts * sizeof(float2)) : 0);
+    s.total = s.scores + (weights ? all * ((bound + kStep - 1) / kStep * kStep) * sizeof(float) : 0);
+    return s;
 }
 
 template <int DP, int KF, int VF>
-void launch_mt(const DecodeArgs& a, const Plan& p, hipStream_t st)
+void launch_tiles(const DecodeArgs& a, const Plan& p, hipStream_t st)
 {
     const dim3 grid((unsigned)p.parts, (unsigned)(a.c.kv_heads * p.chunks), (unsigned)a.c.sequences);
-    if (p.MT == 1) decode_kernel<DP, KF, VF, 1><<<grid, 64 * kWaves, 0, st>>>(a, a.c.block_table, a.c.k_range, a.c.v_range);
-    else decode_kernel<DP, KF, VF, 2><<<grid, 64 * kWaves, 0, st>>>(a, a.c.block_table, a.c.k_range, a.c.v_range);
+    const int32_t* table = a.c.block_table;
+    const float *kr = a.c.k_range, *vr = a.c.v_range;
+    if (p.MT == 1) decode_kernel<DP, KF, VF, 1><<<grid, 64 * kWaves, 0, st>>>(a, table, kr, vr);
+    else decode_kernel<DP, KF, VF, 2><<<grid, 64 * kWaves, 0, st>>>(a, table, kr, vr);
 }
 
 template <int DP>
-void launch_forms(const DecodeArgs& a, const Plan& p, hipStream_t st)
+int launch_width(const DecodeArgs& a, const Plan& p, hipStream_t st)
 {
     const bool k8 = a.c.k_form == MNNQ_KV_FP8, v8 = a.c.v_form == MNNQ_KV_FP8;
-    if (k8 && v8) launch_mt<DP, MNNQ_KV_FP8, MNNQ_KV_FP8>(a, p, st);
-    else if (k8) launch_mt<DP, MNNQ_KV_FP8, MNNQ_KV_INT8>(a, p, st);
-    else if (v8) launch_mt<DP, MNNQ_KV_INT8, MNNQ_KV_FP8>(a, p, st);
-    else launch_mt<DP, MNNQ_KV_INT8, MNNQ_KV_INT8>(a, p, st);
+    if (k8 && v8) launch_tiles<DP, MNNQ_KV_FP8, MNNQ_KV_FP8>(a, p, st);
+    else if (k8) launch_tiles<DP, MNNQ_KV_FP8, MNNQ_KV_INT8>(a, p, st);
+    else if (v8) launch_tiles<DP, MNNQ_KV_INT8, MNNQ_KV_FP8>(a, p, st);
+    else launch_tiles<DP, MNNQ_KV_INT8, MNNQ_KV_INT8>(a, p, st);
+    MNNQ_HIP_TRY(hipGetLastError());
+    const int64_t joins = p.parts > 1 ? a.rows : 0, given = a.weights ? (a.bound + kJoinThreads - 1) / kJoinThreads : 0;
+    if (joins + given > 0) {
+        join_kernel<DP><<<dim3((unsigned)(joins + given), (unsigned)a.c.kv_heads, (unsigned)a.c.sequences), kJoinThreads, 0, st>>>(a);
+        MNNQ_HIP_TRY(hipGetLastError());
+    }
+    return MNNQ_OK;
 }
 
 }  // namespace
 
 size_t attn_decode_ws_bytes(const mnnq_kv_cache& c, int64_t tokens, int heads, int64_t bound, bool weights)
 {
-    const Plan p = plan_of(c, tokens, heads, bound, weights);
-    const int64_t rows = heads / c.kv_heads * tokens;
-    return part_bytes(c, p, rows, weights) + (weights ? round16((size_t)(c.sequences * c.kv_heads * rows * bound) * 4) : 0);
+    return space_of(c, plan_of(c, tokens, heads, bound), heads / c.kv_heads * tokens, bound, weights).total;
 }
 
 int launch_attn_decode(const mnnq_kv_cache& c, bool bf16, int64_t tokens, int heads, int64_t bound, float scale,
                        const Rows& q, const Rows& out, float* weights, int64_t weights_stride, void* workspace,
                        hipStream_t st)
 {
-    const Plan p = plan_of(c, tokens, heads, bound, weights != nullptr);
-    DecodeArgs a;
+    const Plan p = plan_of(c, tokens, heads, bound);
+    DecodeArgs a{};
     a.c = c;
     a.q = q;
     a.out = out;
+    a.weights = weights;
+    a.weights_stride = weights_stride;
     a.tokens = tokens;
-    a.bound = bound;
+    a.bound = (int)bound;
     a.part_len = p.part_len;
     a.parts = p.parts;
-    a.heads = heads;
+    a.scores_stride = (bound + kStep - 1) / kStep * kStep;
     a.group = heads / c.kv_heads;
     a.rows = (int)(a.group * tokens);
     a.scale_log2 = scale * kLog2e;
     a.bf16 = bf16;
-    a.part = p.parts > 1 || weights ? static_cast<float*>(workspace) : nullptr;
-    a.scores = weights ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + part_bytes(c, p, a.rows, true)) : nullptr;
-    if (p.DP == 64) launch_forms<64>(a, p, st);
-    else if (p.DP == 128) launch_forms<128>(a, p, st);
-    else launch_forms<256>(a, p, st);
-    MNNQ_HIP_TRY(hipGetLastError());
-    if (p.parts > 1) {
-        const dim3 grid((unsigned)a.rows, (unsigned)c.kv_heads, (unsigned)c.sequences);
-        if (p.DP == 64) join_kernel<64><<<grid, 256, 0, st>>>(a);
-        else if (p.DP == 128) join_kernel<128><<<grid, 256, 0, st>>>(a);
-        else join_kernel<256><<<grid, 256, 0, st>>>(a);
-        MNNQ_HIP_TRY(hipGetLastError());
-    }
-    if (weights) {
-        const dim3 grid((unsigned)((bound + 255) / 256), (unsigned)c.kv_heads, (unsigned)c.sequences);
-        weights_kernel<<<grid, 256, 0, st>>>(a, weights, weights_stride, p.DP);
-        MNNQ_HIP_TRY(hipGetLastError());
-    }
-    return MNNQ_OK;
+    const Space sp = space_of(c, p, a.rows, bound, weights != nullptr);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.sums = p.parts > 1 ? reinterpret_cast<float*>(ws) : nullptr;
+    a.stats = p.parts > 1 || weights ? reinterpret_cast<float2*>(ws + sp.stats) : nullptr;
+    a.scores = weights ? reinterpret_cast<float*>(ws + sp.scores) : nullptr;
+    return p.DP == 64 ? launch_width<64>(a, p, st) : p.DP == 128 ? launch_width<128>(a, p, st) : launch_width<256>(a, p, st);
 }
 
 }  // namespace mnnq
