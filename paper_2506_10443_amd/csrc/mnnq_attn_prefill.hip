@@ -7,6 +7,8 @@
 #include "mnnq_attn.h"
 #include "mnnq_forms.h"
 
+#include <type_traits>
+
 namespace mnnq {
 
 namespace {
@@ -46,6 +48,12 @@ constexpr float kSlack = 8.0f;                   // the running maximum follows 
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef short s8v __attribute__((ext_vector_type(8)));
 
+// All but the youngest N of this wave's direct loads are in LDS; its LDS reads are done; they are, and everybody's.
+template <int N = 0>
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // 16 bytes per lane from base + off, zeros where that is not below `bytes`, to at + 16 lane.
 __device__ __forceinline__ void load_to_lds(const void* base, int64_t bytes, uint8_t* at, int off)
 {
@@ -68,129 +76,170 @@ __device__ __forceinline__ bool holds_no_number(const uint8_t* tile, int lane)
     return __ballot(top.x >= kFirst || top.y >= kFirst) != 0;
 }
 
-template <int DP, bool BF16, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void prefill_kernel(PrefillArgs a)
+// Two transposing reads.  (The compiler would wait in front of them for every direct load in flight, also for those of other tiles;
+// pointers that alias nothing else here leave the waits to landed().)
+__device__ __forceinline__ s8v read_transposed(const uint8_t* __restrict__ a, const uint8_t* __restrict__ b, const int* __restrict__)
 {
-    using T = Type<BF16>;
-    typedef typename T::V8 V8;
-    constexpr int BM = 32 * NW;
-    constexpr int CH = DP / 8;                   // 16-byte units of a row
-    constexpr int kTileBytes = kTile * DP * 2;
-    constexpr int kLoads = kTileBytes / 1024 / NW;
-    extern __shared__ __align__(16) uint8_t lds[];   // K0 K1 V0 V1
+    const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)a);
+    const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)b);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 31, half = lane >> 5;
-    // tile of queries and head
+// Order of a stretch of code: LDS reads, AHEAD of the matrix instructions they feed, EACH behind one, for N / 2 of N.
+template <int AHEAD, int EACH, int N>
+__device__ __forceinline__ void pace()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i < N / 2) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    }
+}
+
+// What a workgroup works on: BM queries of a head and the keys they see.
+struct Work {
+    Span q, k;
+    int64_t q0;                                  // first query, in the sequence
+    int64_t shift;                               // query i sees the keys up to i + shift
+    int head, kvh;
+    int tiles, full;                             // tiles of keys that some query sees; that all queries see all of
+};
+
+template <int BM>
+__device__ __forceinline__ bool find_work(const PrefillArgs& a, Work& w)
+{
+    // Long rows first.  Workgroup b runs on XCD b % 8: where that fits, the heads that share keys are on one XCD.
     const int64_t tile_id = a.tiles - 1 - blockIdx.x / a.heads;
-    const int head = blockIdx.x % a.heads, kvh = head / (a.heads / a.kv_heads);
-    int64_t s = 0;
-    {   // sequence s owns the tiles from q_start[s] / BM + s on: n queries fill at most n / BM + 1
-        int64_t lo = 0, hi = a.sequences - 1;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi + 1) >> 1;
-            const int64_t at = a.q_start[mid], in = at < 0 ? 0 : at > a.q_tokens ? a.q_tokens : at;
-            if (in / BM + mid <= tile_id) lo = mid;
-            else hi = mid - 1;
-        }
-        s = lo;
+    w.head = blockIdx.x % a.heads;
+    if (a.heads % kXcdCount == 0) w.head = w.head % kXcdCount * (a.heads / kXcdCount) + w.head / kXcdCount;
+    w.kvh = w.head / (a.heads / a.kv_heads);
+    // Sequence s owns the tiles from q_start[s] / BM + s on: n queries fill at most n / BM + 1.
+    int64_t lo = 0, hi = a.sequences - 1;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        const int64_t at = a.q_start[mid], in = at < 0 ? 0 : at > a.q_tokens ? a.q_tokens : at;
+        if (in / BM + mid <= tile_id) lo = mid;
+        else hi = mid - 1;
     }
-    const Span qs = span_of(a.q_start, s, a.q_tokens), ks = span_of(a.k_start, s, a.k_tokens);
-    const int64_t q0 = (tile_id - (qs.begin / BM + s)) * BM;
-    if (q0 < 0 || q0 >= qs.count) return;
-    const int64_t shift = ks.count - qs.count;   // query i sees the keys up to i + shift
-    const int64_t q_end = q0 + BM < qs.count ? q0 + BM : qs.count;
-    int64_t n_keys = q_end + shift;              // seen by the last query here
-    n_keys = n_keys < 0 ? 0 : n_keys;
-    const int n_tiles = (int)((n_keys + kTile - 1) / kTile);
-    const int64_t mine = q0 + wave * 32 + col;   // this lane's query
-    const bool there = mine < qs.count;
-    const int64_t limit = there ? mine + shift + 1 : 0;      // keys below it are seen
-    const int64_t wave_low = q0 + wave * 32 + shift + 1;     // seen by all queries of the wave
-    const int64_t wave_high = q0 + wave * 32 + 32 + shift;   // by the last one
+    w.q = span_of(a.q_start, lo, a.q_tokens);
+    w.k = span_of(a.k_start, lo, a.k_tokens);
+    w.q0 = (tile_id - (w.q.begin / BM + lo)) * BM;
+    if (w.q0 < 0 || w.q0 >= w.q.count) return false;
+    w.shift = w.k.count - w.q.count;
+    const int64_t q_end = w.q0 + BM < w.q.count ? w.q0 + BM : w.q.count;
+    const int64_t keys = q_end + w.shift < 0 ? 0 : q_end + w.shift;
+    w.tiles = (int)((keys + kTile - 1) / kTile);
+    const int64_t by_all = w.q0 + w.shift + 1 < 0 ? 0 : (w.q0 + w.shift + 1) / kTile;
+    w.full = by_all < w.tiles ? (int)by_all : w.tiles;
+    return true;
+}
 
-    // queries
-    V8 qf[DP / 16];
+// Place of a row's 16-byte unit u in LDS: u ^ pattern, chosen for each operand so that the lanes which an LDS read serves together
+// touch every bank once.
+template <int DP>
+__device__ __forceinline__ int k_pattern(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
+template <int DP>
+__device__ __forceinline__ int v_pattern(int row) { return DP == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; }
+
+// Direct loads of tiles of keys or values by WAVES waves, each its own part of the rows.
+template <int DP, int WAVES>
+struct Loader {
+    static constexpr int kLoads = kTile * DP * 2 / 1024 / WAVES;
+    const uint16_t* base;
+    int64_t token, rows;
+    int D, wave;
+    int off[kLoads];
+
+    template <typename Pattern>
+    __device__ __forceinline__ Loader(const Rows& x, const Span& span, int head, int D, int wave, int lane, Pattern pattern)
+        : base(x.data + span.begin * x.token + head * x.head), token(x.token), rows(span.count), D(D), wave(wave)
     {
-        const uint16_t* src = a.q.data + (qs.begin + (there ? mine : q0)) * a.q.token + head * a.q.head + 8 * half;
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            u4v w = {0, 0, 0, 0};
-            if (there && 16 * i + 8 * half < a.D) w = *reinterpret_cast<const u4v*>(src + 16 * i);
-            qf[i] = __builtin_bit_cast(V8, w);
-        }
-    }
-
-    // Direct loads: unit u of a tile's row lies at place u ^ (row's pattern), chosen for each operand so that the lanes which an
-    // LDS read serves together touch every bank once.
-    auto k_pattern = [](int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; };
-    auto v_pattern = [](int row) { return DP == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; };
-    const uint16_t* k_base = a.k.data + ks.begin * a.k.token + kvh * a.k.head;
-    const uint16_t* v_base = a.v.data + ks.begin * a.v.token + kvh * a.v.head;
-    int k_off[kLoads], v_off[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int unit = (wave * kLoads + i) * 64 + lane, row = unit / CH, at = unit % CH;
-        const int ku = at ^ k_pattern(row), vu = at ^ v_pattern(row);
-        k_off[i] = ku * 8 < a.D ? (int)(row * a.k.token + ku * 8) * 2 : kOutOfRange;
-        v_off[i] = vu * 8 < a.D ? (int)(row * a.v.token + vu * 8) * 2 : kOutOfRange;
-    }
-    auto tile_bytes = [&](int64_t token, int64_t first) {
-        const int64_t rows = ks.count - first < kTile ? ks.count - first : kTile;
-        return ((rows - 1) * token + a.D) * 2;
-    };
-    auto issue = [&](int t, int slot) {
-        const int64_t first = (int64_t)t * kTile;
-        const uint16_t* kp = k_base + first * a.k.token;
-        const uint16_t* vp = v_base + first * a.v.token;
-        const int64_t kn = tile_bytes(a.k.token, first), vn = tile_bytes(a.v.token, first);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            load_to_lds(kp, kn, lds + slot * kTileBytes + (wave * kLoads + i) * 1024, k_off[i]);
-            load_to_lds(vp, vn, lds + (2 + slot) * kTileBytes + (wave * kLoads + i) * 1024, v_off[i]);
+            const int unit = (wave * kLoads + i) * 64 + lane, row = unit / (DP / 8), u = (unit % (DP / 8)) ^ pattern(row);
+            off[i] = u * 8 < D ? (int)(row * token + u * 8) * 2 : kOutOfRange;
         }
-    };
-
-    f16v o[DP / 32];
+    }
+    __device__ __forceinline__ void load(int t, uint8_t* to) const
+    {
+        const int64_t first = (int64_t)t * kTile, left = rows - first < kTile ? rows - first : kTile;
+        const uint16_t* from = base + first * token;
+        const int64_t bytes = ((left - 1) * token + D) * 2;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
-    float mx = kLowest, l = 0.0f;                // mx: of the scores times scale_log2; l: of this lane's tokens
+        for (int i = 0; i < kLoads; ++i) load_to_lds(from, bytes, to + (wave * kLoads + i) * 1024, off[i]);
+    }
+};
 
-    if (n_tiles > 0) issue(0, 0);
-    for (int t = 0; t < n_tiles; ++t) {
-        const int slot = t & 1;
-        __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): the tile is here, the one before is read
-        __builtin_amdgcn_s_barrier();
-        if (t + 1 < n_tiles) issue(t + 1, slot ^ 1);
-        const int64_t first = (int64_t)t * kTile;
-        if (first >= wave_high) continue;        // no query of this wave sees the tile
-        const uint8_t* kt = lds + slot * kTileBytes;
-        const uint8_t* vt = lds + (2 + slot) * kTileBytes;
-        f16v sc[2];
+// A wave's 32 queries: lane (half, col) holds of query col the scores of keys 8 i + 4 half + {0..3} of a tile and the results
+// d = 8 i + 4 half + {0..3}.
+template <int DP, bool BF16>
+struct Queries {
+    using T = Type<BF16>;
+    typedef typename T::V8 V8;
+    int lane, col, half;
+    int64_t limit;                               // this lane's query sees the keys below
+    float scale;                                 // of the scores, log2
+    bool there;
+    V8 qf[DP / 16];
+    f16v o[DP / 32];
+    float mx, l;                                 // maximum of the scores times scale; sum over this lane's keys
+
+    __device__ __forceinline__ Queries(const PrefillArgs& a, const Work& w, int lane, int64_t first)
+        : lane(lane), col(lane & 31), half(lane >> 5), scale(a.scale_log2), mx(kLowest), l(0.0f)
+    {
+        const int64_t mine = first + col;
+        there = mine < w.q.count;
+        limit = there ? mine + w.shift + 1 : 0;
+        const uint16_t* src = a.q.data + (w.q.begin + (there ? mine : 0)) * a.q.token + w.head * a.q.head + 8 * half;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            u4v x = {0, 0, 0, 0};
+            if (there && 16 * i + 8 * half < a.D) x = *reinterpret_cast<const u4v*>(src + 16 * i);
+            qf[i] = __builtin_bit_cast(V8, x);
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
+    }
+
+    // S^T = K Q^T of a tile.
+    __device__ __forceinline__ void scores(const uint8_t* kt, f16v (&sc)[2]) const
+    {
+        V8 kf[2][DP / 16];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const int row = 32 * j + col;
+                kf[j][i] = *reinterpret_cast<const V8*>(kt + row * DP * 2 + (((2 * i + half) ^ k_pattern<DP>(row)) << 4));
+            }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             sc[j] = f16v{};
-            const int row = 32 * j + col;
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                const V8 kf = *reinterpret_cast<const V8*>(kt + row * DP * 2 + (((2 * i + half) ^ k_pattern(row)) << 4));
-                sc[j] = T::mfma(kf, qf[i], sc[j]);
-            }
+            for (int i = 0; i < DP / 16; ++i) sc[j] = T::mfma(kf[j][i], qf[i], sc[j]);
         }
-        const bool masked = first + kTile > wave_low;
-        if (masked) {
+    }
+
+    // Probabilities of the tile that begins with key `first`.
+    template <bool MASKED>
+    __device__ __forceinline__ void probabilities(f16v (&sc)[2], int64_t first, V8 (&pf)[4])
+    {
+        if (MASKED) {
+            const int left = (int)(limit - first < kTile ? limit - first : kTile);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (first + 32 * j + 8 * (e / 4) + 4 * half + e % 4 >= limit) sc[j][e] = -__builtin_inff();
+                    if (32 * j + 8 * (e / 4) + 4 * half + e % 4 >= left) sc[j][e] = -__builtin_inff();
         }
         float top = sc[0][0];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[j][e]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        const u2v other = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])) * scale;
         // the maximum follows only when it is far behind: probabilities stay below 2^kSlack
         if (__ballot(top > mx + kSlack)) {
             const float now = fmaxf(mx, top);
@@ -201,7 +250,6 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void prefill_kernel(Prefi
             for (int i = 0; i < DP / 32; ++i) o[i] *= down;
         }
         const float less = T::kLift - mx;
-        V8 pf[4];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -209,77 +257,197 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void prefill_kernel(Prefi
                 u4v w;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x], a.scale_log2, less));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x + 1], a.scale_log2, less));
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x], scale, less));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x + 1], scale, less));
                     l += p0;
                     l += p1;
                     w[x] = pack16(p0, p1, BF16);
                 }
                 pf[2 * j + e / 8] = __builtin_bit_cast(V8, w);
             }
-        // four tokens of a row of V^T per read: the 16 lanes of a group address 4 tokens x 16 values
-        auto read_v = [&](int ks16, int i) {
-            const int row = 16 * ks16 + 4 * half + ((lane & 15) >> 2);
-            const int unit = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const uint8_t* at = vt + row * DP * 2 + ((unit ^ v_pattern(row)) << 4) + (lane & 1) * 8;
-            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)at);
-            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)(at + 8 * DP * 2));
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        if (masked && holds_no_number<DP, BF16>(vt, lane)) {
+    }
+
+    // Four keys of a row of V^T per read: the 16 lanes of a group address 4 keys x 16 values.
+    __device__ __forceinline__ s8v read_v(const uint8_t* vt, int ks16, int i) const
+    {
+        const int row = 16 * ks16 + 4 * half + ((lane & 15) >> 2);
+        const int unit = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        const uint8_t* at = vt + row * DP * 2 + ((unit ^ v_pattern<DP>(row)) << 4) + (lane & 1) * 8;
+        return read_transposed(at, at + 8 * DP * 2, nullptr);
+    }
+
+    // O^T += V^T P^T of the tile that begins with key `first`.
+    template <bool MASKED>
+    __device__ __forceinline__ void values(const uint8_t* vt, const V8 (&pf)[4], int64_t first)
+    {
+        if (MASKED && holds_no_number<DP, BF16>(vt, lane)) {
             // 0 * inf: a product over all keys would carry what a query must not see into its row.  The numbers first; then the
-            // others token by token, and only the columns that see the token take the result.
+            // others key by key, and only the columns that see the key take the result.
             constexpr short kFirst = BF16 ? 0x7f80 : 0x7c00;
 #pragma unroll
             for (int ks16 = 0; ks16 < 4; ++ks16)
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i) {
-                    s8v x = read_v(ks16, i);
+                    s8v x = read_v(vt, ks16, i);
                     x = (x & 0x7fff) >= kFirst ? 0 : x;
                     o[i] = T::mfma(__builtin_bit_cast(V8, x), pf[ks16], o[i]);
                 }
+            const V8 p0 = pf[0], p1 = pf[1], p2 = pf[2], p3 = pf[3];
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
 #pragma nounroll
-            for (int j = 0; j < kTile; ++j) {
-                const int e = (j & 3) + 4 * ((j >> 3) & 1);
-                const bool seen = first + j < limit;
-                V8 pj = pf[0];
-                pj = j >= 16 ? pf[1] : pj;
-                pj = j >= 32 ? pf[2] : pj;
-                pj = j >= 48 ? pf[3] : pj;
+                for (int j = 0; j < kTile; ++j) {
+                    const V8 pj = j < 32 ? (j < 16 ? p0 : p1) : (j < 48 ? p2 : p3);
+                    // (the key's value: element e of the lanes of one half)
+                    const int e = half == ((j >> 2) & 1) ? (j & 3) + 4 * ((j >> 3) & 1) : -1;
+                    s8v one = read_v(vt, j >> 4, i);
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    s8v one = read_v(j >> 4, i);
-                    one = (one & 0x7fff) >= kFirst ? one : 0;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        if (x != e || half != ((j >> 2) & 1)) one[x] = 0;
+                    for (int x = 0; x < 8; ++x) one[x] = x == e && (one[x] & 0x7fff) >= kFirst ? one[x] : 0;
                     const f16v with = T::mfma(__builtin_bit_cast(V8, one), pj, o[i]);
+                    const bool seen = first + j < limit;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) o[i][x] = seen ? with[x] : o[i][x];
                 }
-            }
-            continue;
+            return;
         }
 #pragma unroll
         for (int ks16 = 0; ks16 < 4; ++ks16)
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) o[i] = T::mfma(__builtin_bit_cast(V8, read_v(ks16, i)), pf[ks16], o[i]);
+            for (int i = 0; i < DP / 32; ++i) o[i] = T::mfma(__builtin_bit_cast(V8, read_v(vt, ks16, i)), pf[ks16], o[i]);
     }
 
-    l += __shfl_xor(l, 32);
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    if (!there) return;
-    uint16_t* to = a.out.data + (qs.begin + mine) * a.out.token + head * a.out.head + 4 * half;
+    __device__ __forceinline__ void store(const PrefillArgs& a, const Work& w, int64_t first)
+    {
+        const float sum = l + __shfl_xor(l, 32);
+        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+        if (!there) return;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
+        for (int i = 0; i < DP / 32; ++i) store_block(a, w, first, i, o[i], inv);
+    }
+
+    // Results 32 i .. 32 i + 31 of the query, times inv.
+    __device__ __forceinline__ void store_block(const PrefillArgs& a, const Work& w, int64_t first, int i, const f16v& x, float inv) const
+    {
+        uint16_t* to = a.out.data + (w.q.begin + first + col) * a.out.token + w.head * a.out.head + 4 * half;
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int d = 32 * i + 2 * e;
-            if (d < a.D) {
-                const u2v w = {pack16(o[i][e] * inv, o[i][e + 1] * inv, BF16), pack16(o[i][e + 2] * inv, o[i][e + 3] * inv, BF16)};
-                *reinterpret_cast<u2v*>(to + d) = w;
-            }
+            if (d < a.D)
+                *reinterpret_cast<u2v*>(to + d) = u2v{pack16(x[e] * inv, x[e + 1] * inv, BF16),
+                                                      pack16(x[e + 2] * inv, x[e + 3] * inv, BF16)};
         }
+    }
+};
+
+// NW waves of 32 queries each, the next tile in flight while one is worked on.
+template <int DP, bool BF16, int NW>
+__global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void prefill_kernel(PrefillArgs a)
+{
+    constexpr int kTileBytes = kTile * DP * 2;
+    extern __shared__ __align__(16) uint8_t lds[];   // K0 K1 V0 V1
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Work w;
+    if (!find_work<32 * NW>(a, w)) return;
+    const int64_t first = w.q0 + wave * 32;
+    const Loader<DP, NW> keys(a.k, w.k, w.kvh, a.D, wave, lane, k_pattern<DP>);
+    const Loader<DP, NW> vals(a.v, w.k, w.kvh, a.D, wave, lane, v_pattern<DP>);
+    auto issue = [&](int t) {
+        keys.load(t, lds + (t & 1) * kTileBytes);
+        vals.load(t, lds + (2 + (t & 1)) * kTileBytes);
+    };
+    if (w.tiles > 0) issue(0);
+    Queries<DP, BF16> q(a, w, lane, first);
+    auto tile = [&](int t, auto masked) {
+        f16v sc[2];
+        typename Type<BF16>::V8 pf[4];
+        q.scores(lds + (t & 1) * kTileBytes, sc);
+        pace<DP / 16, 1, DP / 8>();
+        q.template probabilities<decltype(masked)::value>(sc, (int64_t)t * kTile, pf);
+        q.template values<decltype(masked)::value>(lds + (2 + (t & 1)) * kTileBytes, pf, (int64_t)t * kTile);
+        if (!decltype(masked)::value) pace<DP / 8, 2, DP / 8>();
+    };
+    auto arrived = [&](int t) {
+        landed();
+        meet();
+        if (t + 1 < w.tiles) issue(t + 1);
+    };
+    int t = 0;
+    for (; t < w.full; ++t) {
+        arrived(t);
+        tile(t, std::false_type{});
+    }
+    for (; t < w.tiles; ++t) {
+        arrived(t);
+        if ((int64_t)t * kTile < first + 32 + w.shift) tile(t, std::true_type{});     // (else no query of this wave sees it)
+    }
+    q.store(a, w, first);
+}
+
+// NW waves on the same 32 queries, each with every NW-th tile of keys and room for one tile of its own: for calls with so few queries
+// that tiles of queries leave CUs idle.  A wave requests its next keys when it has read the ones before, values likewise; the waves
+// join through LDS.
+template <int DP, bool BF16, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a)
+{
+    constexpr int kTileBytes = kTile * DP * 2, NV = DP / 32;
+    extern __shared__ __align__(16) uint8_t lds[];   // K and V of wave 0, of wave 1, ...; then the waves' sums and statistics
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Work w;
+    if (!find_work<32>(a, w)) return;
+    uint8_t* const kt = lds + wave * 2 * kTileBytes;
+    uint8_t* const vt = kt + kTileBytes;
+    const Loader<DP, 1> keys(a.k, w.k, w.kvh, a.D, 0, lane, k_pattern<DP>);
+    const Loader<DP, 1> vals(a.v, w.k, w.kvh, a.D, 0, lane, v_pattern<DP>);
+    if (wave < w.tiles) keys.load(wave, kt), vals.load(wave, vt);
+    Queries<DP, BF16> q(a, w, lane, w.q0);
+    auto tile = [&](int t, auto masked) {
+        f16v sc[2];
+        typename Type<BF16>::V8 pf[4];
+        landed<Loader<DP, 1>::kLoads>();             // (all but the values behind them)
+        q.scores(kt, sc);
+        read();
+        const bool more = t + NW < w.tiles;
+        if (more) keys.load(t + NW, kt);
+        q.template probabilities<decltype(masked)::value>(sc, (int64_t)t * kTile, pf);
+        if (more) landed<Loader<DP, 1>::kLoads>();
+        else landed<0>();
+        q.template values<decltype(masked)::value>(vt, pf, (int64_t)t * kTile);
+        read();
+        if (more) vals.load(t + NW, vt);
+    };
+    int t = wave;
+    for (; t < w.full; t += NW) tile(t, std::false_type{});
+    for (; t < w.tiles; t += NW) tile(t, std::true_type{});
+
+    // Join: block i of the results (d = 32 i ..) is summed and stored by wave i % NW.
+    float* const sums = reinterpret_cast<float*>(lds);
+    float* const stats = sums + NW * DP * 32;
+    meet();
+    const float l = q.l + __shfl_xor(q.l, 32);
+    if (q.half == 0) stats[wave * 64 + q.col] = q.mx, stats[wave * 64 + 32 + q.col] = l;
+    meet();
+    float top = stats[q.col], sum = 0.0f;
+#pragma unroll
+    for (int x = 1; x < NW; ++x) top = fmaxf(top, stats[x * 64 + q.col]);
+#pragma unroll
+    for (int x = 0; x < NW; ++x) sum += stats[x * 64 + 32 + q.col] * __builtin_amdgcn_exp2f(stats[x * 64 + q.col] - top);
+    const float down = __builtin_amdgcn_exp2f(q.mx - top);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[((wave * NV + i) * 16 + e) * 64 + lane] = q.o[i][e] * down;
+    meet();
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i % NW != wave) continue;
+        f16v o = {};
+#pragma unroll
+        for (int x = 0; x < NW; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] += sums[((x * NV + i) * 16 + e) * 64 + lane];
+        if (q.there) q.store_block(a, w, w.q0, i, o, inv);
+    }
 }
 
 template <int DP, bool BF16, int NW>
@@ -294,9 +462,30 @@ int launch_waves(PrefillArgs& a, hipStream_t st)
     return MNNQ_OK;
 }
 
+template <int DP, bool BF16, int NW>
+int launch_split(PrefillArgs& a, hipStream_t st)
+{
+    constexpr size_t kTiles = NW * 2 * (size_t)kTile * DP * 2, kJoin = NW * (DP * 32 + 64) * sizeof(float);
+    constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
+    static thread_local int allowed = -1;
+    if (int e = allow_large_lds(prefill_split_kernel<DP, BF16, NW>, kLds, allowed)) return e;
+    a.tiles = a.q_tokens / 32 + a.sequences;
+    prefill_split_kernel<DP, BF16, NW><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW, kLds, st>>>(a);
+    MNNQ_HIP_TRY(hipGetLastError());
+    return MNNQ_OK;
+}
+
 template <int DP, bool BF16>
 int launch_type(PrefillArgs& a, hipStream_t st)
 {
+    // By the number of 32-query blocks there may be.  Up to one per CU: four waves share a block's keys; up to four: two; else four
+    // waves have a block each and share tiles of keys.  Measured in us, 4 waves a block / 2 / a block each: 204 blocks (512 tokens, 12
+    // heads) 9.4 / 10.7 / 16.7; 84 (64 queries behind 2048 keys, 28 heads) 20.5 / 25.4 / 39.9; 476 16.4 / 12.7 / 18.1; 924 34.5 /
+    // 23.2 / 28.4; 2080 93.9 / 65.6 / 52.3; 2296 (twenty of 100) 58.8 / 35.1 / 28.3.  (256 wide, LDS holds the tiles of two.)
+    const int64_t blocks = (a.q_tokens / 32 + a.sequences) * a.heads;
+    if constexpr (DP < 256)
+        if (blocks <= 256) return launch_split<DP, BF16, 4>(a, st);
+    if (blocks <= 1152) return launch_split<DP, BF16, 2>(a, st);
     return launch_waves<DP, BF16, 4>(a, st);
 }
 
