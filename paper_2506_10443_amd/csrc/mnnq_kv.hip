@@ -71,94 +71,122 @@ __device__ __forceinline__ bool find_piece(const AppendArgs& a, int64_t p, Piece
     return true;
 }
 
-// A power of two that keeps a product with TOP finite (bfloat16 goes to 3.4e38); what it takes below the normal numbers has
-// codes of zero against such a range.
-__device__ __forceinline__ float headroom(float range) { return range > 0x1p100f ? 0x1p-64f : 1.0f; }
+// Quotients n / range, correctly rounded, three operations each: q = n inv, q + (n - q range) inv with inv = 1 / range correctly
+// rounded (Markstein's theorem; a range is a number of 11 bits at most, not one of all ones).  Range and numerators are scaled by a power of
+// two that brings the range to [1, 2), or as near as one such factor can, so that nothing on the way leaves the normal numbers.
+struct Divisor {
+    float scale, range, inv;
+    __device__ __forceinline__ explicit Divisor(float r)
+    {
+        const int e = (int)((__float_as_uint(r) >> 23) & 255u) - 127;
+        const int up = min(-e, 118);            // (2^118 * 448 is still a number)
+        scale = __uint_as_float((uint32_t)max(up + 127, 1) << 23);
+        range = r * scale;
+        inv = 1.0f / range;
+    }
+    // n: a numerator times `scale`
+    __device__ __forceinline__ float operator()(float n) const
+    {
+        const float q = n * inv;
+        return __builtin_fmaf(__builtin_fmaf(-range, q, n), inv, q);
+    }
+};
 
-// Sixteen codes of a range `before` as codes of the range `range`.
+// Sixteen codes of a range `before` as codes of the divisor's range.
 template <int FORM>
-__device__ __forceinline__ uint4 recode16(uint4 w, float before, float range)
+__device__ __forceinline__ uint4 recode16(uint4 w, float before, const Divisor& by)
 {
-    const float room = headroom(range), from = before * room, to = range * room;
+    const float from = before * by.scale;
     uint32_t d[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float c[4];
         codes_to_float<FORM>(d[j], c);
-        d[j] = codes_of<FORM>(c[0] * from / to, c[1] * from / to, c[2] * from / to, c[3] * from / to);
+        d[j] = codes_of<FORM>(by(c[0] * from), by(c[1] * from), by(c[2] * from), by(c[3] * from));
     }
     return uint4{d[0], d[1], d[2], d[3]};
 }
 
-template <int FORM>
-__device__ __forceinline__ uint2 encode8(uint4 x, float range, bool bf16)
+// Eight values as codes of the divisor's range.
+template <int FORM, bool BF16>
+__device__ __forceinline__ uint2 encode8(const uint4& x, const Divisor& by)
 {
-    const float room = headroom(range), to = range * room;
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    const float up = by.scale * code_top<FORM>();
     uint32_t out[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         float y[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t bits = j & 1 ? w[2 * i + j / 2] >> 16 : w[2 * i + j / 2] & 0xffffu;
-            y[j] = value16(bits, bf16) * room * code_top<FORM>() / to;
-        }
+        for (int j = 0; j < 4; ++j)
+            y[j] = by(value16(j & 1 ? w[2 * i + j / 2] >> 16 : w[2 * i + j / 2] & 0xffffu, BF16) * up);
         out[i] = codes_of<FORM>(y[0], y[1], y[2], y[3]);
     }
     return uint2{out[0], out[1]};
 }
 
-template <int FORM, int THREADS>
-__device__ void append_piece(const AppendArgs& a, const Piece& p, const Rows& x, uint8_t* codes, float* ranges, int head)
+// R: 16-byte pieces of the new rows that a thread holds, THREADS * R at least in all.
+template <int FORM, int THREADS, int R>
+__device__ __forceinline__ void append_piece(const AppendArgs& a, const Piece& p, const Rows& x, uint8_t* codes, float* ranges,
+                                             int head)
 {
+    typedef unsigned short us2v __attribute__((ext_vector_type(2)));
     __shared__ uint32_t wave_top[THREADS / 64];
     const int tid = threadIdx.x, D = a.c.head_dim, per_row = D / 8;
-    const int chunks = p.count * per_row;
     const uint16_t* src = x.data + p.row * x.token + head * x.head;
     const int64_t slot = p.block * a.c.kv_heads + head;
     uint8_t* dst = codes + slot * a.c.block_tokens * D;
     const float before = p.first > 0 ? ranges[slot] : 0.0f;
-    // greatest magnitude: of the bits without the sign, as integers (a NaN is above every number)
-    uint32_t top = 0;
-    for (int i = tid; i < chunks; i += THREADS) {
-        const int row = i / per_row, ch = i - row * per_row;
-        const uint4 w = *reinterpret_cast<const uint4*>(src + row * x.token + ch * 8);
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    uint4 w[R];
+    int to[R];                                   // the piece's place among the codes; -1: none
+    int row = tid / per_row, ch = tid - row * per_row;
+    const int row_step = THREADS / per_row, ch_step = THREADS - row_step * per_row;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = v[j] & 0x7fffu, hi = (v[j] >> 16) & 0x7fffu;
-            top = max(top, max(lo, hi));
-        }
+    for (int i = 0; i < R; ++i) {
+        to[i] = row < p.count ? (p.first + row) * D + ch * 8 : -1;
+        w[i] = uint4{0, 0, 0, 0};
+        if (row < p.count) w[i] = *reinterpret_cast<const uint4*>(src + row * x.token + ch * 8);
+        row += row_step, ch += ch_step;
+        if (ch >= per_row) ch -= per_row, ++row;
     }
+    // greatest magnitude: of the bits without the sign, as integers (a NaN is above every number)
+    us2v two = {0, 0};
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) two = __builtin_elementwise_max(two, __builtin_bit_cast(us2v, v[j] & 0x7fff7fffu));
+    }
+    uint32_t top = max((uint32_t)two.x, (uint32_t)two.y);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
     if (THREADS > 64) {
         if ((tid & 63) == 0) wave_top[tid >> 6] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) top = max(top, wave_top[w]);
+        for (int i = 0; i < THREADS / 64; ++i) top = max(top, wave_top[i]);
     }
-    const float fresh = value16(top, a.bf16);
     // (as integers too: magnitudes, and a NaN stays one)
-    const float range = __uint_as_float(max(__float_as_uint(fresh), __float_as_uint(before) & 0x7fffffffu));
-    if (p.first > 0 && __float_as_uint(range) != __float_as_uint(before)) {
+    const float range = __uint_as_float(max(__float_as_uint(value16(top, a.bf16)), __float_as_uint(before) & 0x7fffffffu));
+    const Divisor by(range);
+    if (p.first > 0 && __float_as_uint(range) != __float_as_uint(before))
         for (int i = tid; i < p.first * D / 16; i += THREADS) {
             uint4* at = reinterpret_cast<uint4*>(dst + i * 16);
-            *at = recode16<FORM>(*at, before, range);
+            *at = recode16<FORM>(*at, before, by);
         }
-    }
-    for (int i = tid; i < chunks; i += THREADS) {
-        const int row = i / per_row, ch = i - row * per_row;
-        const uint4 w = *reinterpret_cast<const uint4*>(src + row * x.token + ch * 8);
-        const uint2 q = range > 0.0f || range != range ? encode8<FORM>(w, range, a.bf16) : uint2{0, 0};
-        *reinterpret_cast<uint2*>(dst + (p.first + row) * D + ch * 8) = q;
-    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (to[i] >= 0) {
+            uint2 q = {0, 0};
+            if (__float_as_uint(range) != 0)
+                q = a.bf16 ? encode8<FORM, true>(w[i], by) : encode8<FORM, false>(w[i], by);
+            *reinterpret_cast<uint2*>(dst + to[i]) = q;
+        }
     if (tid == 0) ranges[slot] = range;
 }
 
 // One workgroup per block that rows go to, head, and K or V.
-template <int THREADS>
+template <int THREADS, int R>
 __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
 {
     Piece p;
@@ -168,8 +196,8 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
     const Rows& x = is_v ? a.v : a.k;
     uint8_t* codes = static_cast<uint8_t*>(is_v ? a.c.v_codes : a.c.k_codes);
     float* ranges = is_v ? a.c.v_range : a.c.k_range;
-    if ((is_v ? a.c.v_form : a.c.k_form) == MNNQ_KV_FP8) append_piece<MNNQ_KV_FP8, THREADS>(a, p, x, codes, ranges, head);
-    else append_piece<MNNQ_KV_INT8, THREADS>(a, p, x, codes, ranges, head);
+    if ((is_v ? a.c.v_form : a.c.k_form) == MNNQ_KV_FP8) append_piece<MNNQ_KV_FP8, THREADS, R>(a, p, x, codes, ranges, head);
+    else append_piece<MNNQ_KV_INT8, THREADS, R>(a, p, x, codes, ranges, head);
 }
 
 // ---- evict
@@ -210,148 +238,192 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kDigits[3] = {11, 11, 10};         // bits of a key that a pass settles, from the top
 
-// One workgroup per sequence and key head: the key of the last token that is kept by a radix search of four passes, then the
-// kept tokens in order.
+// One workgroup per sequence and key head: the key of the last token that is kept by a radix search of three passes over the
+// keys, then the kept tokens in order.  Wave w has the tokens from w * per_wave on, 64 at a time; R: keys that a thread holds (0: they
+// are read again in every pass).
+template <int R>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 {
-    __shared__ int hist[256];
-    __shared__ int wave_sum[2][kSelectThreads / 64];
-    __shared__ uint32_t sh_prefix;
+    constexpr int kUnroll = R > 0 ? R : 1;
+    __shared__ int hist[2048];
+    __shared__ int wave_sum[kSelectWaves], wave_equal[kSelectWaves], wave_above[kSelectWaves];
+    __shared__ uint32_t sh_digit;
     __shared__ int sh_need;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int head = blockIdx.x;
     const int64_t s = blockIdx.y;
-    const int64_t len = evict_length(a, s), n = evict_kept(a, len);
+    const int len = (int)evict_length(a, s), n = (int)evict_kept(a, len);
     const int64_t row = s * a.c.kv_heads + head;
     const float* w = a.weights + row * a.weights_stride;
     int32_t* kept = a.kept + row * a.keep;
     float* nw = a.new_weights + row * a.new_weights_stride;
-    const int64_t last = a.recent < n ? a.recent : n;        // kept as the newest
-    const int64_t old = len - last;                          // the others compete
-    int need = (int)(n - last);                              // for this many places
+    const int last = a.recent < n ? (int)a.recent : n;       // kept as the newest
+    const int old = len - last;                              // the others compete
+    const int places = n - last;                             // for this many places
+    const int steps = (len + kSelectThreads - 1) / kSelectThreads, first = wave * steps * 64 + lane;
+    const int most = R > 0 ? R : steps;                      // (a bound that loops over held keys are unrolled by)
+    float held[kUnroll];
+    if (R > 0)
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j) held[j] = j < steps && first + j * 64 < len ? w[first + j * 64] : 0.0f;
+    auto weight = [&](int j) { return R > 0 ? held[R > 0 ? j : 0] : first + j * 64 < len ? w[first + j * 64] : 0.0f; };
+
+    // prefix: the settled bits of the last kept key; need: places left for keys that have them
     uint32_t prefix = 0;
-    if (need > 0 && need < old) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
+    int need = places, shift = 32;
+    if (places > 0 && places < old)
+        for (int pass = 0; pass < 3; ++pass) {
+            const int bits = kDigits[pass], above = shift;
+            shift -= bits;
+            for (int i = tid; i < 2048; i += kSelectThreads) hist[i] = 0;
             __syncthreads();
-            for (int64_t i = tid; i < old; i += kSelectThreads) {
-                const uint32_t key = weight_key(w[i]);
-                if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1);
+#pragma unroll kUnroll
+            for (int j = 0; j < most; ++j) {
+                if (j >= steps) continue;
+                const uint32_t key = weight_key(weight(j));
+                if (first + j * 64 < old && (pass == 0 || key >> above == prefix >> above))
+                    atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1);
             }
             __syncthreads();
-            if (tid == 0) {
-                int left = need, b = 255;
-                while (b > 0 && hist[b] < left) left -= hist[b--];
-                sh_prefix = prefix | (uint32_t)b << shift;
-                sh_need = left;
+            // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
+            const int b0 = hist[2047 - 2 * tid], b1 = hist[2046 - 2 * tid];
+            int sum = b0 + b1;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const int other = __shfl_up(sum, m);
+                if (lane >= m) sum += other;
+            }
+            if (lane == 63) wave_sum[wave] = sum;
+            __syncthreads();
+            int before = sum - b0 - b1;
+#pragma unroll
+            for (int x = 0; x < kSelectWaves; ++x) before += x < wave ? wave_sum[x] : 0;
+            if (before < need && before + b0 + b1 >= need) {
+                const bool second = before + b0 < need;
+                sh_digit = 2047 - 2 * tid - (second ? 1 : 0);
+                sh_need = need - before - (second ? b0 : 0);
             }
             __syncthreads();
-            prefix = sh_prefix;
-            need = sh_need;                                  // places left for keys with this prefix
+            prefix |= sh_digit << shift;
+            need = sh_need;
             __syncthreads();
         }
+    // All where there are places for all, else the keys above the prefix, and of those that equal it the first `need`.
+    const bool all = places >= old, none = places <= 0;
+    auto above = [&](int j) {
+        const int i = first + j * 64;
+        return (i >= old && i < len) || (i < old && !none && (all || weight_key(weight(j)) > prefix));
+    };
+    auto equal = [&](int j) { return first + j * 64 < old && !none && !all && weight_key(weight(j)) == prefix; };
+    int n_above = 0, n_equal = 0;
+#pragma unroll kUnroll
+    for (int j = 0; j < most; ++j) {
+        if (j >= steps) continue;
+        n_above += __popcll(__ballot(above(j)));
+        n_equal += __popcll(__ballot(equal(j)));
     }
-    // above the prefix: kept; equal to it: the first `need`; all of them where there are places for all.
-    const bool all = n - last >= old, none = n - last <= 0;
-    int64_t done = 0;
-    int equal_before = 0;
-    for (int64_t base = 0; base < len; base += kSelectThreads) {
-        const int64_t i = base + tid;
-        const uint32_t key = i < old ? weight_key(w[i]) : 0;
-        const bool competes = i < old && !none;
-        const bool equal = competes && !all && key == prefix;
-        const uint64_t eq = __ballot(equal);
-        if (lane == 0) wave_sum[0][wave] = __popcll(eq);
-        __syncthreads();
-        int rank = equal_before + __popcll(eq & (((uint64_t)1 << lane) - 1));
-        int eq_total = 0;
-        for (int j = 0; j < kSelectThreads / 64; ++j) {
-            if (j < wave) rank += wave_sum[0][j];
-            eq_total += wave_sum[0][j];
-        }
-        equal_before += eq_total;
-        const bool take = (i >= old && i < len) || (competes && (all || key > prefix)) || (equal && rank < need);
+    if (lane == 0) wave_above[wave] = n_above, wave_equal[wave] = n_equal;
+    __syncthreads();
+    int at = 0, equal_before = 0;
+#pragma unroll
+    for (int x = 0; x < kSelectWaves; ++x)
+        if (x < wave) at += wave_above[x], equal_before += wave_equal[x];
+    at += equal_before < need ? equal_before : need;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll kUnroll
+    for (int j = 0; j < most; ++j) {
+        if (j >= steps) continue;
+        const bool is_equal = equal(j);
+        const uint64_t eq = __ballot(is_equal);
+        const bool take = above(j) || (is_equal && equal_before + __popcll(eq & below) < need);
         const uint64_t tk = __ballot(take);
-        if (lane == 0) wave_sum[1][wave] = __popcll(tk);
-        __syncthreads();
-        int64_t at = done + __popcll(tk & (((uint64_t)1 << lane) - 1));
-        for (int j = 0; j < kSelectThreads / 64; ++j) {
-            if (j < wave) at += wave_sum[1][j];
-            done += wave_sum[1][j];
+        const int to = at + __popcll(tk & below);
+        if (take && to < n) {
+            kept[to] = first + j * 64;
+            nw[to] = weight(j);
         }
-        if (take && at < n) {
-            kept[at] = (int32_t)i;
-            nw[at] = w[i];
-        }
+        equal_before += __popcll(eq);
+        at += __popcll(tk);
     }
     for (int64_t i = n + tid; i < a.keep; i += kSelectThreads) kept[i] = -1;
     for (int64_t i = n + tid; i < a.new_weights_stride; i += kSelectThreads) nw[i] = 0.0f;
-    if (head == 0 && tid == 0) a.new_lengths[s] = (int32_t)n;
+    if (head == 0 && tid == 0) a.new_lengths[s] = n;
 }
 
 constexpr int kMoveThreads = 256;
+constexpr int kMovePieces = 4;                   // 16-byte pieces of K, and of V, that a thread has in flight
 
-template <int FORM>
-__device__ void move_block(const EvictArgs& a, const int32_t* kept, int count, int64_t s, int head, int64_t to, uint8_t* codes,
-                           float* ranges, int64_t* from, float* range_of, float& sh_top)
-{
-    const int tid = threadIdx.x, D = a.c.head_dim, B = a.c.block_tokens;
-    // where each token lies, and its range
-    for (int i = tid; i < count; i += kMoveThreads) {
-        const int64_t t = kept[i];
-        const int64_t block = a.c.block_table[s * a.c.table_blocks + t / B];
-        const bool there = block >= 0 && block < a.c.blocks;
-        const int64_t at = block * a.c.kv_heads + head;
-        from[i] = there ? (at * B + t % B) * D : -1;
-        range_of[i] = there ? ranges[at] : 0.0f;
-    }
-    __syncthreads();
-    if (tid < 64) {
-        uint32_t top = 0;
-        for (int i = tid; i < count; i += 64) top = max(top, __float_as_uint(range_of[i]) & 0x7fffffffu);
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
-        if (tid == 0) sh_top = __uint_as_float(top);
-    }
-    __syncthreads();
-    const float range = sh_top;
-    uint8_t* dst = codes + (to * a.c.kv_heads + head) * B * D;
-    const int per_row = D / 16;
-    for (int i = tid; i < count * per_row; i += kMoveThreads) {
-        const int r = i / per_row;
-        uint4 w = {0, 0, 0, 0};
-        if (from[r] >= 0) w = *reinterpret_cast<const uint4*>(codes + from[r] + (i - r * per_row) * 16);
-        const float before = range_of[r];
-        if (__float_as_uint(before) != __float_as_uint(range)) w = recode16<FORM>(w, before, range);
-        *reinterpret_cast<uint4*>(dst + i * 16) = w;
-    }
-    if (tid == 0) ranges[to * a.c.kv_heads + head] = range;
-}
-
-// One workgroup per new block, key head, and K or V.
+// One workgroup per new block and key head.
+template <int KF, int VF>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
 {
     __shared__ int64_t from[128];
-    __shared__ float range_of[128];
-    __shared__ float sh_top;
+    __shared__ float range_of[2][128];
+    const int tid = threadIdx.x, lane = tid & 63, D = a.c.head_dim, B = a.c.block_tokens;
     const int64_t s = blockIdx.z, b = blockIdx.x;
-    const int head = blockIdx.y >> 1;
-    const bool is_v = blockIdx.y & 1;
-    const int64_t n = evict_kept(a, evict_length(a, s));
-    const int64_t first = b * a.c.block_tokens;
-    if (first >= n) return;
-    const int count = (int)(n - first < a.c.block_tokens ? n - first : a.c.block_tokens);
+    const int head = blockIdx.y;
+    const int32_t* kept = a.kept + (s * a.c.kv_heads + head) * a.keep + b * B;
+    // (the length, the new block and the first of the places are requested together)
+    const int32_t early = tid < B && b * B + tid < a.keep ? kept[tid] : -1;
     const int64_t to = a.new_table[s * a.new_table_blocks + b];
-    if (to < 0 || to >= a.c.blocks) return;
-    const int32_t* kept = a.kept + (s * a.c.kv_heads + head) * a.keep + first;
-    uint8_t* codes = static_cast<uint8_t*>(is_v ? a.c.v_codes : a.c.k_codes);
-    float* ranges = is_v ? a.c.v_range : a.c.k_range;
-    if ((is_v ? a.c.v_form : a.c.k_form) == MNNQ_KV_FP8)
-        move_block<MNNQ_KV_FP8>(a, kept, count, s, head, to, codes, ranges, from, range_of, sh_top);
-    else
-        move_block<MNNQ_KV_INT8>(a, kept, count, s, head, to, codes, ranges, from, range_of, sh_top);
+    const int64_t left = evict_kept(a, evict_length(a, s)) - b * B;
+    if (left <= 0 || to < 0 || to >= a.c.blocks) return;
+    const int count = (int)(left < B ? left : B);
+    // where each token lies, and its ranges
+    if (tid < count) {
+        const int64_t block = a.c.block_table[s * a.c.table_blocks + early / B];
+        const bool there = block >= 0 && block < a.c.blocks;
+        const int64_t at = (there ? block : 0) * a.c.kv_heads + head;
+        from[tid] = there ? (at * B + early % B) * D : -1;
+        range_of[0][tid] = there ? a.c.k_range[at] : 0.0f;
+        range_of[1][tid] = there ? a.c.v_range[at] : 0.0f;
+    }
+    __syncthreads();
+    // (magnitudes as integers; a NaN stays one)
+    uint32_t top[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        top[x] = lane < count ? __float_as_uint(range_of[x][lane]) & 0x7fffffffu : 0u;
+        if (lane + 64 < count) top[x] = max(top[x], __float_as_uint(range_of[x][lane + 64]) & 0x7fffffffu);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top[x] = max(top[x], (uint32_t)__shfl_xor((int)top[x], m));
+    }
+    uint8_t* const codes[2] = {static_cast<uint8_t*>(a.c.k_codes), static_cast<uint8_t*>(a.c.v_codes)};
+    const int64_t slot = to * a.c.kv_heads + head;
+    const Divisor by_k(__uint_as_float(top[0])), by_v(__uint_as_float(top[1]));
+    const int per_row = D / 16, pieces = count * per_row;
+    for (int base = tid; base < pieces; base += kMoveThreads * kMovePieces) {
+        uint4 k[kMovePieces], v[kMovePieces];
+        int r[kMovePieces];
+#pragma unroll
+        for (int i = 0; i < kMovePieces; ++i) {
+            const int at = base + i * kMoveThreads;
+            r[i] = at < pieces ? at / per_row : -1;
+            k[i] = v[i] = uint4{0, 0, 0, 0};
+            if (r[i] >= 0 && from[r[i]] >= 0) {
+                const int64_t source = from[r[i]] + (at - r[i] * per_row) * 16;
+                k[i] = *reinterpret_cast<const uint4*>(codes[0] + source);
+                v[i] = *reinterpret_cast<const uint4*>(codes[1] + source);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kMovePieces; ++i) {
+            if (r[i] < 0) continue;
+            const float kb = range_of[0][r[i]], vb = range_of[1][r[i]];
+            if (__float_as_uint(kb) != top[0]) k[i] = recode16<KF>(k[i], kb, by_k);
+            if (__float_as_uint(vb) != top[1]) v[i] = recode16<VF>(v[i], vb, by_v);
+            const int64_t place = slot * B * D + (int64_t)(base + i * kMoveThreads) * 16;
+            *reinterpret_cast<uint4*>(codes[0] + place) = k[i];
+            *reinterpret_cast<uint4*>(codes[1] + place) = v[i];
+        }
+    }
+    if (tid == 0) {
+        a.c.k_range[slot] = __uint_as_float(top[0]);
+        a.c.v_range[slot] = __uint_as_float(top[1]);
+    }
 }
 
 }  // namespace
@@ -369,8 +441,11 @@ int launch_kv_append(const mnnq_kv_cache& c, bool bf16, const int32_t* start, in
         pieces = a.pieces_each * c.sequences;
     }
     const dim3 grid((unsigned)pieces, (unsigned)(2 * c.kv_heads));
-    if (!start && a.each == 1) append_kernel<64><<<grid, 64, 0, st>>>(a);
-    else append_kernel<256><<<grid, 256, 0, st>>>(a);
+    // the most 16-byte pieces of a block, head and kind that come at once
+    const int64_t rows = !start && a.each < c.block_tokens ? a.each : c.block_tokens, most = rows * (c.head_dim / 8);
+    if (most <= 64) append_kernel<64, 1><<<grid, 64, 0, st>>>(a);
+    else if (most <= 1024) append_kernel<256, 4><<<grid, 256, 0, st>>>(a);
+    else append_kernel<256, 16><<<grid, 256, 0, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
     return MNNQ_OK;
 }
@@ -381,11 +456,19 @@ int launch_kv_evict(const mnnq_kv_cache& c, const float* weights, int64_t weight
 {
     const EvictArgs a{c,    weights,     weights_stride, keep,        recent,            new_table, new_table_blocks,
                       kept, new_lengths, new_weights,    new_weights_stride};
-    select_kernel<<<dim3((unsigned)c.kv_heads, (unsigned)c.sequences), kSelectThreads, 0, st>>>(a);
+    const dim3 rows((unsigned)c.kv_heads, (unsigned)c.sequences);
+    const int64_t room = c.table_blocks * c.block_tokens, most = room < weights_stride ? room : weights_stride;
+    if (most <= 4 * kSelectThreads) select_kernel<4><<<rows, kSelectThreads, 0, st>>>(a);
+    else if (most <= 16 * kSelectThreads) select_kernel<16><<<rows, kSelectThreads, 0, st>>>(a);
+    else select_kernel<0><<<rows, kSelectThreads, 0, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
-    const int64_t room = new_table_blocks, most = (keep + c.block_tokens - 1) / c.block_tokens;
-    const dim3 grid((unsigned)(room < most ? room : most), (unsigned)(2 * c.kv_heads), (unsigned)c.sequences);
-    move_kernel<<<grid, kMoveThreads, 0, st>>>(a);
+    const int64_t needed = (keep + c.block_tokens - 1) / c.block_tokens;
+    const dim3 grid((unsigned)(new_table_blocks < needed ? new_table_blocks : needed), (unsigned)c.kv_heads, (unsigned)c.sequences);
+    const bool k8 = c.k_form == MNNQ_KV_FP8, v8 = c.v_form == MNNQ_KV_FP8;
+    if (k8 && v8) move_kernel<MNNQ_KV_FP8, MNNQ_KV_FP8><<<grid, kMoveThreads, 0, st>>>(a);
+    else if (k8) move_kernel<MNNQ_KV_FP8, MNNQ_KV_INT8><<<grid, kMoveThreads, 0, st>>>(a);
+    else if (v8) move_kernel<MNNQ_KV_INT8, MNNQ_KV_FP8><<<grid, kMoveThreads, 0, st>>>(a);
+    else move_kernel<MNNQ_KV_INT8, MNNQ_KV_INT8><<<grid, kMoveThreads, 0, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
     return MNNQ_OK;
 }
