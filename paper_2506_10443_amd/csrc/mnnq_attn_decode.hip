@@ -478,17 +478,21 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
     for (int base = 0; base < a.rows; base += kRowsAtOnce) {
         const int rows = a.rows - base < kRowsAtOnce ? a.rows - base : kRowsAtOnce;
         __syncthreads();
-        for (int r = wave; r < rows; r += kJoinThreads / 64) {
+        // sixteen lanes per row
+        for (int r = tid / 16; r < rows; r += kJoinThreads / 16) {
             const float2* st = a.stats + (row0 + base + r) * a.parts;
-            float top = kLowest, l = 0.0f;
-            for (int i = lane; i < n; i += 64) top = fmaxf(top, st[i].x);
+            const int i0 = tid & 15;
+            const float2 mine = i0 < n ? st[i0] : float2{kLowest, 0.0f};
+            float top = mine.x;
+            for (int i = i0 + 16; i < n; i += 16) top = fmaxf(top, st[i].x);
 #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-            for (int i = lane; i < n; i += 64) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - top);
+            for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+            float l = mine.y * __builtin_amdgcn_exp2f(mine.x - top);
+            for (int i = i0 + 16; i < n; i += 16) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - top);
 #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) l += __shfl_xor(l, m);
+            for (int m = 1; m < 16; m <<= 1) l += __shfl_xor(l, m);
             // (a row that sees nothing gives nothing)
-            if (lane == 0) row_top[r] = top - kTopBits, row_inv[r] = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            if (i0 == 0) row_top[r] = top - kTopBits, row_inv[r] = l > 0.0f || l != l ? 1.0f / l : 0.0f;
         }
         __syncthreads();
         if (t < len) {
