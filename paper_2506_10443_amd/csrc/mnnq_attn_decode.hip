@@ -518,17 +518,20 @@ Plan plan_of(const mnnq_kv_cache& c, int64_t tokens, int heads, int64_t bound)
     p.MT = rows > 16 ? 2 : 1;
     p.chunks = (rows + 16 * p.MT - 1) / (16 * p.MT);
     const int64_t base = c.sequences * c.kv_heads * p.chunks;
-    // One sequence: a workgroup per CU, of 128 tokens at least.  Several, of lengths that only the device knows: three per CU, so
-    // that short ones leave no CU idle, of 256 tokens at least (256 wide, where a CU holds one: one).  Measured in us, 256 / 512 / 768
-    // workgroups: 16384 tokens of 8 key heads 13.9 / 14.8 / 14.8, 131072 of 4 33.3 / 33.6 / 34.0; 32 ragged sequences of up to
-    // 6045 61.4 / 53.0 / 49.8; 4 of 8000, 256 wide, 21.4 / 28.3 / 28.4.  Least tokens 128 / 256: 1001 tokens of 4 key heads
-    // 8.4 / 9.5; 8 sequences with weights 19.8 / 18.0.
-    const int64_t most = (c.sequences > 1 && p.DP < 256 ? 768 : 256) / base, least = c.sequences > 1 ? 256 : 128;
+    // One sequence: a workgroup per CU, of 128 tokens at least.  Several, of lengths that only the device knows: five per CU, so that
+    // what the short ones leave idle is little, of 256 tokens at least (256 wide, where a CU holds one: one).  Measured in us, 256 / 512 /
+    // 768 workgroups: 16384 tokens of 8 key heads 13.9 / 14.8 / 14.8, 131072 of 4 33.3 / 33.6 / 34.0; 4 sequences of 8000, 256 wide,
+    // 21.4 / 28.3 / 28.4.  768 / 1280 / 2048: 32 ragged sequences of up to 6045 49.8 / 45.0 / 59.2, 24 of up to 8000 54.4 / 47.6 / 47.9,
+    // 64 of up to 4000, 4 key heads, 37.7 / 34.3 / 45.3, 8 of 8000 32.7 / 32.5 / 35.4.  (Parts sized on the device from the lengths
+    // themselves: 45.5, 45.5, 33.8, 35.3, and 1.5 more for one sequence: its chain is longer.)  Least tokens 128 / 256: 1001 tokens of 4
+    // key heads 8.4 / 9.5; 8 sequences with weights 19.8 / 18.0.
+    const int64_t most = (c.sequences > 1 && p.DP < 256 ? 1280 : 256) / base, least = c.sequences > 1 ? 256 : 128;
     const int64_t want = most > 0 ? most : 1;
     int64_t part = (bound + want - 1) / want;
     if (part < least) part = least;
-    // (up to 512 tokens one part, without the second kernel, is faster: 300 tokens 7.7 against 8.6 us)
-    if (bound <= 512) part = bound;
+    // One part, without the second kernel: up to 512 tokens (300 tokens 7.7 against 8.6 us), and two workgroups per CU that are not
+    // long (64 sequences of 1000 tokens, 8 key heads, 28.9 against 35.7).
+    if (bound <= 512 || (base >= 512 && bound <= 2048)) part = bound;
     const int64_t whole = kWaves * kStep;
     part = (part + whole - 1) / whole * whole;
     if (part * kMaxParts < bound) part = (bound + kMaxParts * whole - 1) / (kMaxParts * whole) * whole;
