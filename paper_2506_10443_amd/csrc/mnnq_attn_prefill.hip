@@ -36,11 +36,21 @@ struct Type<true> {
     typedef bf8v V8;
     static __device__ __forceinline__ f16v mfma(V8 a, V8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr float kLift = 0.0f;
+    // l + the two values of a dword, which are summed as the second product uses them: rounded.  One instruction in place of two
+    // additions (packed prompts of up to 1500 tokens, 28 heads, 64 -> 58 us).
+    static __device__ __forceinline__ float add_pair(uint32_t two, float l)
+    {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2v, two), bf2v{(__bf16)1.0f, (__bf16)1.0f}, l, false);
+    }
 };
 template <>
 struct Type<false> {
     typedef half8v V8;
     static __device__ __forceinline__ f16v mfma(V8 a, V8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float add_pair(uint32_t two, float l)
+    {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), half2v{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+    }
     static constexpr float kLift = 6.0f;         // probabilities up to 2^14 (with kSlack) instead of 2^8: halves reach further down
 };
 constexpr float kSlack = 8.0f;                   // the running maximum follows when it is 2^8 behind
@@ -260,9 +270,8 @@ struct Queries {
                 for (int x = 0; x < 4; ++x) {
                     const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x], scale, less));
                     const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e + 2 * x + 1], scale, less));
-                    l += p0;
-                    l += p1;
                     w[x] = pack16(p0, p1, BF16);
+                    l = T::add_pair(w[x], l);
                 }
                 pf[2 * j + e / 8] = __builtin_bit_cast(V8, w);
             }

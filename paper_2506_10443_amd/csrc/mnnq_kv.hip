@@ -238,6 +238,12 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// The weight again (a zero without its sign, a NaN as one of them).
+__device__ __forceinline__ float weight_of(uint32_t key)
+{
+    return __uint_as_float(key == 0xffffffffu ? 0x7fc00000u : key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits[3] = {11, 11, 10};         // bits of a key that a pass settles, from the top
 
@@ -265,27 +271,32 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
     const int places = n - last;                             // for this many places
     const int steps = (len + kSelectThreads - 1) / kSelectThreads, first = wave * steps * 64 + lane;
     const int most = R > 0 ? R : steps;                      // (a bound that loops over held keys are unrolled by)
-    float held[kUnroll];
+    // (0: no token that competes; the keys of numbers and NaN are above it)
+    auto key_at = [&](int j) { return first + j * 64 < old ? weight_key(w[first + j * 64]) : 0u; };
+    uint32_t held[kUnroll];
     if (R > 0)
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) held[j] = j < steps && first + j * 64 < len ? w[first + j * 64] : 0.0f;
-    auto weight = [&](int j) { return R > 0 ? held[R > 0 ? j : 0] : first + j * 64 < len ? w[first + j * 64] : 0.0f; };
+        for (int j = 0; j < kUnroll; ++j) held[j] = j < steps ? key_at(j) : 0u;
+    auto key_of = [&](int j) { return R > 0 ? held[R > 0 ? j : 0] : key_at(j); };
 
-    // prefix: the settled bits of the last kept key; need: places left for keys that have them
-    uint32_t prefix = 0;
-    int need = places, shift = 32;
-    if (places > 0 && places < old)
+    // prefix: the settled bits of the last kept key; need: places left for keys that have them.  All keys are above 0, none above
+    // the greatest.
+    uint32_t prefix = places > 0 ? 0u : 0xffffffffu;
+    int need = 0;
+    if (places > 0 && places < old) {
+        need = places;
+        int shift = 32;
         for (int pass = 0; pass < 3; ++pass) {
             const int bits = kDigits[pass], above = shift;
             shift -= bits;
             for (int i = tid; i < 2048; i += kSelectThreads) hist[i] = 0;
             __syncthreads();
+            const uint32_t settled = pass == 0 ? 0u : prefix >> above, mask = (1u << bits) - 1;
 #pragma unroll kUnroll
             for (int j = 0; j < most; ++j) {
                 if (j >= steps) continue;
-                const uint32_t key = weight_key(weight(j));
-                if (first + j * 64 < old && (pass == 0 || key >> above == prefix >> above))
-                    atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1);
+                const uint32_t key = key_of(j);
+                if (key && (pass == 0 || key >> above == settled)) atomicAdd(&hist[key >> shift & mask], 1);
             }
             __syncthreads();
             // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
@@ -309,21 +320,15 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
             __syncthreads();
             prefix |= sh_digit << shift;
             need = sh_need;
-            __syncthreads();
         }
-    // All where there are places for all, else the keys above the prefix, and of those that equal it the first `need`.
-    const bool all = places >= old, none = places <= 0;
-    auto above = [&](int j) {
-        const int i = first + j * 64;
-        return (i >= old && i < len) || (i < old && !none && (all || weight_key(weight(j)) > prefix));
-    };
-    auto equal = [&](int j) { return first + j * 64 < old && !none && !all && weight_key(weight(j)) == prefix; };
+    }
+    // Kept: the keys above the prefix, of those that equal it the first `need`, and the newest tokens behind them.
     int n_above = 0, n_equal = 0;
 #pragma unroll kUnroll
     for (int j = 0; j < most; ++j) {
         if (j >= steps) continue;
-        n_above += __popcll(__ballot(above(j)));
-        n_equal += __popcll(__ballot(equal(j)));
+        n_above += __popcll(__ballot(key_of(j) > prefix));
+        n_equal += __popcll(__ballot(key_of(j) == prefix));
     }
     if (lane == 0) wave_above[wave] = n_above, wave_equal[wave] = n_equal;
     __syncthreads();
@@ -332,21 +337,27 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
     for (int x = 0; x < kSelectWaves; ++x)
         if (x < wave) at += wave_above[x], equal_before += wave_equal[x];
     at += equal_before < need ? equal_before : need;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    at = __builtin_amdgcn_readfirstlane(at), equal_before = __builtin_amdgcn_readfirstlane(equal_before);
+    auto below = [](uint64_t m) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); };
 #pragma unroll kUnroll
     for (int j = 0; j < most; ++j) {
         if (j >= steps) continue;
-        const bool is_equal = equal(j);
-        const uint64_t eq = __ballot(is_equal);
-        const bool take = above(j) || (is_equal && equal_before + __popcll(eq & below) < need);
+        const uint32_t key = key_of(j);
+        bool take = key > prefix;
+        const uint64_t eq = __ballot(key == prefix);
+        if (eq && equal_before < need) take |= key == prefix && equal_before + below(eq) < need;
         const uint64_t tk = __ballot(take);
-        const int to = at + __popcll(tk & below);
+        const int to = at + below(tk);
         if (take && to < n) {
             kept[to] = first + j * 64;
-            nw[to] = weight(j);
+            nw[to] = weight_of(key);
         }
         equal_before += __popcll(eq);
         at += __popcll(tk);
+    }
+    for (int i = tid; i < last; i += kSelectThreads) {
+        kept[places + i] = old + i;
+        nw[places + i] = w[old + i];
     }
     for (int64_t i = n + tid; i < a.keep; i += kSelectThreads) kept[i] = -1;
     for (int64_t i = n + tid; i < a.new_weights_stride; i += kSelectThreads) nw[i] = 0.0f;
