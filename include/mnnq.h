@@ -9,7 +9,8 @@
  * (output features), G = K / 64 quantization groups along K.
  *
  * Conventions for every call
- *   - Every pointer is a DEVICE pointer, 16-byte aligned, owned by the caller.
+ *   - Every pointer is a DEVICE pointer, 16-byte aligned, owned by the caller.  (The attention calls' arrays of
+ *     int32 and fp32 - indices, lengths, ranges, weights - need 4-byte alignment only.)
  *     The library never allocates, frees or synchronises.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     Calls only enqueue work; buffers must stay valid until the stream has
@@ -46,7 +47,7 @@ typedef enum {
     MNNQ_ERR_SHAPE = -2,       /* M, N or K <= 0, or K not a multiple of the group */
     MNNQ_ERR_UNSUPPORTED = -3, /* group != 64, unknown mode, N not a multiple of 16, or a size limit (see Limits) */
     MNNQ_ERR_SIZE = -4,        /* packed / workspace buffer too small */
-    MNNQ_ERR_ALIGN = -5,       /* a pointer is not 16-byte aligned */
+    MNNQ_ERR_ALIGN = -5,       /* a pointer is not 16-byte aligned (see Conventions) */
     MNNQ_ERR_HIP = -6          /* a HIP call failed; see mnnq_last_hip_error() */
 } mnnq_status;
 
@@ -318,7 +319,7 @@ int mnnq_plan_debug(int what, int64_t M, int64_t N, int64_t K, int group, int mo
  * and above zero.
  * A query that no key is visible to gives a row of zeros.  Softmax statistics and sums are fp32; the
  * probabilities enter the second product rounded to the type of its other operand (prompt: `type`,
- * cache: fp16 with 2^-39 the smallest that counts), the result is rounded once.
+ * cache: fp16, where those below 2^-32 of the row's greatest are lost), the result is rounded once.
  * A NaN or an infinity in q, k or v reaches the rows that see it and no other row.
  * Device arrays of indices are not looked at on the host; what they hold is bounded in the kernels: a
  * sequence's start and end are clamped to the number of rows given (an end before its start is an empty
@@ -396,8 +397,9 @@ int mnnq_attn_decode(const mnnq_kv_cache *cache, int type, int64_t tokens, int h
  * weights: fp32 [sequences, kv_heads, weights_stride], as mnnq_attn_decode adds them up.
  * A new block's range is the greatest range that its tokens' blocks had; codes are rounded to it.
  * kept: int32 [sequences, kv_heads, keep], the kept tokens' old places, -1 behind the last; new_lengths:
- * int32 [sequences]; new_weights: fp32 [sequences, kv_heads, new_weights_stride], the kept tokens' weights,
- * zeros behind the last (stride >= keep; the room behind is for the tokens to come).  recent <= keep;
+ * int32 [sequences]; new_weights: fp32 [sequences, kv_heads, new_weights_stride], the kept tokens' weights
+ * (-0 as 0, every NaN as the same one), zeros behind the last (stride >= keep; the room behind is for the
+ * tokens to come).  recent <= keep;
  * new_table_blocks * block_tokens >= keep, or new lengths are cut to that room. */
 int mnnq_kv_evict(const mnnq_kv_cache *cache, const float *weights, int64_t weights_stride, int64_t keep, int64_t recent,
                   const int32_t *new_table, int64_t new_table_blocks, int32_t *kept, int32_t *new_lengths,

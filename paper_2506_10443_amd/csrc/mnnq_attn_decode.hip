@@ -11,6 +11,11 @@
 //     stay below 2^14 instead of 1, so that a half holds them down to 2^-32 of the greatest.
 // A wave takes 32 tokens at a time, with the codes of its next 32 in flight; the waves of a workgroup share a part of the
 // sequence and join through LDS, the parts are joined by a second kernel.
+//
+// 2 D bytes per token and key head are read once and 4 D rows operations done with them, at most a few dozen per byte: HBM bounds long
+// caches, a chain of launch, ramp and join short ones.  One token (both kernels): 131072 tokens of 4 key heads, 134 MB, 33.3 us, 28 of
+// them the first kernel at 4.8 TB/s (its loads alone 25.5); 32 ragged sequences, 178 MB, 45; 1001 tokens 8.4.  Loads go to registers, not
+// through LDS: each code is used by one lane.
 #include "mnnq_attn.h"
 #include "mnnq_forms.h"
 

@@ -185,7 +185,9 @@ __device__ __forceinline__ void append_piece(const AppendArgs& a, const Piece& p
     if (tid == 0) ranges[slot] = range;
 }
 
-// One workgroup per block that rows go to, head, and K or V.
+// One workgroup per block that rows go to, head, and K or V: range, older codes and new rows are that block's alone, so nothing is
+// shared and nothing is atomic.  The new rows stay in registers between the range and the codes (2 bytes read and 1 written per
+// number): a prompt of 8192 rows, 8 heads, 128 wide, 50 MB, 11.1 us = 4.5 TB/s; one row 3.4, a launch and two dependent loads.
 template <int THREADS, int R>
 __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
 {
@@ -249,7 +251,9 @@ constexpr int kDigits[3] = {11, 11, 10};         // bits of a key that a pass se
 
 // One workgroup per sequence and key head: the key of the last token that is kept by a radix search of three passes over the
 // keys, then the kept tokens in order.  Wave w has the tokens from w * per_wave on, 64 at a time; R: keys that a thread holds (0: they
-// are read again in every pass).
+// are read again in every pass).  Comparing keys pairwise or sorting them would cost more than the three counts of n; one
+// workgroup, since each pass waits for the one before: 4097 tokens 10.7 us, 16 x 8 rows of 16000 21.9, both the chain of barriers
+// and additions to LDS counters, at under a tenth of the rate of memory.
 template <int R>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 {
@@ -367,7 +371,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 constexpr int kMoveThreads = 256;
 constexpr int kMovePieces = 4;                   // 16-byte pieces of K, and of V, that a thread has in flight
 
-// One workgroup per new block and key head.
+// One workgroup per new block and key head.  Ranges first (the greatest of the tokens' old ones), then the codes, moved as they are
+// where old and new range agree.  A copy bounds it: 16 sequences x 8 heads of up to 4096
+// kept tokens, 128 wide, 243 MB read and written, 45-54 us = 4.5-5.3 TB/s.
 template <int KF, int VF>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
 {
