@@ -333,8 +333,9 @@ typedef enum { MNNQ_F16 = 0, MNNQ_BF16 = 1 } mnnq_type;
  * c * r / 448 (fp8: e4m3, 448 its largest number).  r is the greatest magnitude appended to that block and
  * head, so it is a number of `type` exactly; a new value x gets the code round(x * 127 / r), resp. the e4m3
  * number nearest to x * 448 / r, ties to even; a range of zero has codes of zero.  An infinity or a NaN
- * makes the range infinite or NaN, and what its block and head hold undefined (no error, no effect on
- * other blocks and heads). */
+ * makes the range infinite or NaN and the codes of its block and head zeros: the results that see one of
+ * its tokens are NaN (no error, no effect on other blocks and heads).  A cache filled by other means holds
+ * no code that is a NaN. */
 typedef enum { MNNQ_KV_INT8 = 0, MNNQ_KV_FP8 = 1 } mnnq_kv_form;
 
 /* A cache, and the sequences in it.  A HOST structure of device pointers; calls read it before they return.

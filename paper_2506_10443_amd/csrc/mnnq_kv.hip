@@ -92,6 +92,9 @@ struct Divisor {
     }
 };
 
+// Codes of a range that is no number are zeros: a code without a number would reach tokens' rows that do not see it, as 0 * NaN.
+__device__ __forceinline__ bool a_number(uint32_t range) { return range < 0x7f800000u; }
+
 // Sixteen codes of a range `before` as codes of the divisor's range.
 template <int FORM>
 __device__ __forceinline__ uint4 recode16(uint4 w, float before, const Divisor& by)
@@ -169,16 +172,17 @@ __device__ __forceinline__ void append_piece(const AppendArgs& a, const Piece& p
     // (as integers too: magnitudes, and a NaN stays one)
     const float range = __uint_as_float(max(__float_as_uint(value16(top, a.bf16)), __float_as_uint(before) & 0x7fffffffu));
     const Divisor by(range);
+    const bool number = a_number(__float_as_uint(range));
     if (p.first > 0 && __float_as_uint(range) != __float_as_uint(before))
         for (int i = tid; i < p.first * D / 16; i += THREADS) {
             uint4* at = reinterpret_cast<uint4*>(dst + i * 16);
-            *at = recode16<FORM>(*at, before, by);
+            *at = number ? recode16<FORM>(*at, before, by) : uint4{0, 0, 0, 0};
         }
 #pragma unroll
     for (int i = 0; i < R; ++i)
         if (to[i] >= 0) {
             uint2 q = {0, 0};
-            if (__float_as_uint(range) != 0)
+            if (number && __float_as_uint(range) != 0)
                 q = a.bf16 ? encode8<FORM, true>(w[i], by) : encode8<FORM, false>(w[i], by);
             *reinterpret_cast<uint2*>(dst + to[i]) = q;
         }
@@ -430,8 +434,8 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
         for (int i = 0; i < kMovePieces; ++i) {
             if (r[i] < 0) continue;
             const float kb = range_of[0][r[i]], vb = range_of[1][r[i]];
-            if (__float_as_uint(kb) != top[0]) k[i] = recode16<KF>(k[i], kb, by_k);
-            if (__float_as_uint(vb) != top[1]) v[i] = recode16<VF>(v[i], vb, by_v);
+            if (__float_as_uint(kb) != top[0]) k[i] = a_number(top[0]) ? recode16<KF>(k[i], kb, by_k) : uint4{0, 0, 0, 0};
+            if (__float_as_uint(vb) != top[1]) v[i] = a_number(top[1]) ? recode16<VF>(v[i], vb, by_v) : uint4{0, 0, 0, 0};
             const int64_t place = slot * B * D + (int64_t)(base + i * kMoveThreads) * 16;
             *reinterpret_cast<uint4*>(codes[0] + place) = k[i];
             *reinterpret_cast<uint4*>(codes[1] + place) = v[i];

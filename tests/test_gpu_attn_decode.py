@@ -147,6 +147,32 @@ def test_another_heads_undefined_block_does_no_harm():
     assert torch.equal(out[:, :4], clean[:, :4]) and torch.isnan(out[:, 4:]).all()
 
 
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("k_type,v_type", [(I8, I8), (I8, F8), (F8, I8), (F8, F8)])
+@pytest.mark.parametrize("evicted", [False, True])
+def test_queries_before_an_undefined_block_do_not_see_it(what, k_type, v_type, evicted):
+    """Two queries, the last token opens a block: only the second one sees what is no number there."""
+    outs = []
+    for value in (0.0, what):
+        gen = torch.Generator().manual_seed(11)
+        c = Pair(1, 8, 2, 16, 64, k_type, v_type, spare=8)
+        c.append(rows(gen, 48, 2, 64, torch.bfloat16), rows(gen, 48, 2, 64, torch.bfloat16), [48])
+        k, v = rows(gen, 1, 2, 64, torch.bfloat16), rows(gen, 1, 2, 64, torch.bfloat16)
+        k[:, 1] = v[:, 1] = 0
+        k[0, 1, 3] = v[0, 1, 5] = value
+        B.mnnq_kv_append(k.cuda(), v.cuda(), *c.args())
+        q = rows(gen, 2, 8, 64, torch.bfloat16).cuda()
+        table, lengths = c.table, [49]
+        if evicted:
+            table = c.free.view(1, 8)
+            B.mnnq_kv_evict(*c.args(lengths=lengths), torch.ones((1, 2, 128), device="cuda"), 128, 0, table.cuda(),
+                            torch.empty((1, 2, 128), device="cuda"))
+        outs.append(B.mnnq_attn_decode(q, *c.args(lengths=lengths, table=table)))
+    clean, out = outs
+    assert torch.equal(out[0], clean[0]) and torch.isfinite(clean).all()
+    assert torch.equal(out[1, :4], clean[1, :4]) and torch.isnan(out[1, 4:]).all()
+
+
 def test_strided_queries_and_output():
     gen = torch.Generator().manual_seed(6)
     c = filled(gen, [90, 20], 2, 32, 64)

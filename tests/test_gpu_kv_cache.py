@@ -212,10 +212,11 @@ def test_evict_extremes_of_the_weights():
     w[0, 4, 5] = float("-inf")
     w[0, 4, 50:60] = 1e-42                      # subnormal numbers are numbers
     run_evict(c, w, 40, 4, c.free.view(1, 3), 48)
-    w[0, 5, 7] = float("nan")
+    w[0, 5, 77] = float("nan")
     nw = torch.empty((1, 6, 40), device="cuda")
     kept, _ = B.mnnq_kv_evict(*c.args(), w.cuda(), 40, 4, c.free.view(1, 3).cuda(), nw)
-    assert kept[0, 5].tolist() == [*range(35), *range(124, 128), -1][:39] + [127] or 7 in kept[0, 5].tolist()
+    assert kept[0, 5].tolist() == [*range(35), 77, *range(124, 128)]
+    assert torch.isnan(nw[0, 5, 35]) and not nw[0, 5, :35].any()
 
 
 def test_evict_many_tokens():
