@@ -401,7 +401,8 @@ int mnnq_attn_decode(const mnnq_kv_cache *cache, int type, int64_t tokens, int h
  * int32 [sequences]; new_weights: fp32 [sequences, kv_heads, new_weights_stride], the kept tokens' weights
  * (-0 as 0, every NaN as the same one), zeros behind the last (stride >= keep; the room behind is for the
  * tokens to come).  recent <= keep;
- * new_table_blocks * block_tokens >= keep, or new lengths are cut to that room. */
+ * new_table_blocks * block_tokens >= keep, or new lengths are cut to that room.  The arrays written must not
+ * overlap those read. */
 int mnnq_kv_evict(const mnnq_kv_cache *cache, const float *weights, int64_t weights_stride, int64_t keep, int64_t recent,
                   const int32_t *new_table, int64_t new_table_blocks, int32_t *kept, int32_t *new_lengths,
                   float *new_weights, int64_t new_weights_stride, void *stream);

@@ -10,6 +10,7 @@ namespace {
 constexpr int64_t kMaxGridYZ = 65535;
 constexpr int64_t kMaxRows = (int64_t)1 << 31;           // tokens are indexed by int32 arrays
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence in a cache
+constexpr int64_t kMaxGridX = (int64_t)1 << 24;          // workgroups of 256 in x: 2^32 work items at most
 constexpr int64_t kMaxStride = (int64_t)1 << 23;         // 64 rows within 32-bit byte offsets
 
 inline bool misaligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
@@ -90,7 +91,7 @@ int mnnq_attn_prefill(int type, int64_t sequences, const int32_t* q_start, const
     if (sequences <= 0 || q_tokens < 0 || k_tokens < 0 || !(scale > 0.0f) || !isfinite(scale)) return MNNQ_ERR_SHAPE;
     if (int s = check_heads(heads, kv_heads, head_dim)) return s;
     if (sequences >= kMaxRows || q_tokens >= kMaxRows || k_tokens >= kMaxRows) return MNNQ_ERR_UNSUPPORTED;
-    if ((q_tokens / 32 + sequences) * heads >= kMaxRows) return MNNQ_ERR_UNSUPPORTED;      // workgroups of a launch
+    if (q_tokens / 128 + sequences >= kMaxGridX / heads) return MNNQ_ERR_UNSUPPORTED;       // workgroups of a launch
     const int64_t strides[4][2] = {{q_token, q_head}, {k_token, k_head}, {v_token, v_head}, {out_token, out_head}};
     for (const auto& r : strides)
         if (int s = check_rows(r[0], r[1])) return s;
@@ -110,7 +111,7 @@ int mnnq_kv_append(const mnnq_kv_cache* cache, int type, const int32_t* start, i
     if (tokens > 0 && (!k || !v)) return MNNQ_ERR_NULL;
     if (int s = check_type(type)) return s;
     if (tokens < 0 || (!start && tokens % cache->sequences != 0)) return MNNQ_ERR_SHAPE;
-    if (tokens >= kMaxRows) return MNNQ_ERR_UNSUPPORTED;
+    if (tokens >= kMaxRows || tokens / cache->block_tokens + 2 * cache->sequences >= kMaxGridX) return MNNQ_ERR_UNSUPPORTED;
     if (int s = check_rows(k_token, k_head)) return s;
     if (int s = check_rows(v_token, v_head)) return s;
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(start, 4)) return MNNQ_ERR_ALIGN;
@@ -155,11 +156,13 @@ int mnnq_kv_evict(const mnnq_kv_cache* cache, const float* weights, int64_t weig
     if (!weights || !new_table || !kept || !new_lengths || !new_weights) return MNNQ_ERR_NULL;
     if (keep <= 0 || recent < 0 || recent > keep || weights_stride <= 0 || new_table_blocks <= 0) return MNNQ_ERR_SHAPE;
     if (new_weights_stride < keep) return MNNQ_ERR_SIZE;
-    if (keep > kMaxTokens || new_table_blocks > kMaxTokens / cache->block_tokens || 2 * cache->kv_heads > kMaxGridYZ)
+    if (keep > kMaxTokens || keep / cache->block_tokens >= kMaxGridX || new_table_blocks > kMaxTokens / cache->block_tokens)
         return MNNQ_ERR_UNSUPPORTED;
     if (misaligned(weights, 4) || misaligned(new_table, 4) || misaligned(kept, 4) || misaligned(new_lengths, 4) ||
         misaligned(new_weights, 4))
         return MNNQ_ERR_ALIGN;
+    // in place, one workgroup would write what another still reads
+    if (new_table == cache->block_table || new_lengths == cache->lengths || new_weights == weights) return MNNQ_ERR_UNSUPPORTED;
     return launch_kv_evict(*cache, weights, weights_stride, keep, recent, new_table, new_table_blocks, kept, new_lengths,
                            new_weights, new_weights_stride, static_cast<hipStream_t>(stream));
 }

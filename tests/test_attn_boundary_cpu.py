@@ -104,6 +104,24 @@ def test_evict_refusals(L):
     assert call(stride=0) == SHAPE and call(nstride=63) == SIZE
 
 
+def test_evict_in_place_is_refused(L):
+    c = cache(block_table=FAKE + 64, lengths=FAKE + 128)
+
+    def call(table=FAKE, lengths=FAKE, nw=FAKE + 192):
+        return L.mnnq_kv_evict(ctypes.byref(c), FAKE, 128, 64, 8, table, 2, FAKE, lengths, nw, 64, None)
+
+    assert call(table=FAKE + 64) == call(lengths=FAKE + 128) == call(nw=FAKE) == UNSUPPORTED
+
+
+def test_launches_beyond_the_grid_are_refused(L):
+    """A launch has fewer than 2^32 work items along an axis."""
+    assert L.mnnq_attn_prefill(*{**PREFILL, "q_tokens": 1 << 30, "heads": 64}.values()) == UNSUPPORTED
+    assert L.mnnq_attn_prefill(*{**PREFILL, "sequences": 1 << 23, "heads": 4}.values()) == UNSUPPORTED
+    c = ctypes.byref(cache(block_tokens=16, table_blocks=1 << 25))
+    assert L.mnnq_kv_append(c, 0, None, 1 << 28, FAKE, 128, 64, FAKE, 128, 64, None) == UNSUPPORTED
+    assert L.mnnq_kv_evict(c, FAKE, 1 << 29, 1 << 28, 8, FAKE + 4, 1 << 24, FAKE, FAKE + 4, FAKE + 4, 1 << 28, None) == UNSUPPORTED
+
+
 def test_python_checks_before_the_call():
     """Arrays that are no arrays for the call never reach it (tensors on the CPU are refused by type, whatever their shape)."""
     q = torch.zeros(2, 4, 64, dtype=torch.float16)
