@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             top = column_max(top);
             const bool follow = __ballot(top > mx[m] + kSlack) != 0;
             if (follow || less_unit != 1.0f) {
-                const float now = follow ? fmaxf(mx[m], top) : mx[m];
+                const float now = top > mx[m] + kSlack ? top : mx[m];        // (each row by itself: its bits do not depend on the others)
                 const float down = __builtin_amdgcn_exp2f(mx[m] - now);
                 mx[m] = now;
                 l[m] *= down;

@@ -253,7 +253,7 @@ struct Queries {
         top = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])) * scale;
         // the maximum follows only when it is far behind: probabilities stay below 2^kSlack
         if (__ballot(top > mx + kSlack)) {
-            const float now = fmaxf(mx, top);
+            const float now = top > mx + kSlack ? top : mx;      // (each row by itself: its bits do not depend on the others)
             const float down = __builtin_amdgcn_exp2f(mx - now);
             mx = now;
             l *= down;
@@ -349,53 +349,95 @@ struct Queries {
     }
 };
 
-// NW waves of 32 queries each, the next tile in flight while one is worked on (two tiles of K and V in LDS, 64 KB at 128 wide: two
-// workgroups per CU, whose waves share the matrix cores and the vector units).  4 D operations per visible pair and head, and as many
+// NW 32-query blocks, KS waves on each with every KS-th tile of keys, the next tile in flight while one is worked on; the KS join through
+// LDS.  (KS = 1: two tiles of K and V in LDS, 64 KB at 128 wide: two
+// workgroups per CU, whose waves share the matrix cores and the vector units.  KS = 2: one workgroup, for half as many steps.)  4 D operations per visible pair and head, and as many
 // instructions on scores as matrix ones: what bounds it is the two of them by turns.  One prompt of 8192, 32 heads on 8, 128 wide:
 // 516-548 us, 1.00-1.06 PFLOP/s, matrix cores busy half of the cycles and vector issue a little less; a large matrix product
 // reaches 1.39.  Packed prompts of up to 1500 tokens, 28 heads on 4: 56 us.  64 queries a wave (half the LDS reads) spills:
 // 589-637; eight waves in two halves that take turns at the matrix cores: no faster.
-template <int DP, bool BF16, int NW>
-__global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void prefill_kernel(PrefillArgs a)
+template <int DP, bool BF16, int NW, int KS>
+__global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kernel(PrefillArgs a)
 {
-    constexpr int kTileBytes = kTile * DP * 2;
-    extern __shared__ __align__(16) uint8_t lds[];   // K0 K1 V0 V1
+    static_assert(KS == 1 || KS == 2);
+    constexpr int kTileBytes = kTile * DP * 2, NV = DP / 32;
+    extern __shared__ __align__(16) uint8_t lds[];   // of each part K0 K1 V0 V1; then sums and statistics
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = wave % NW, part = wave / NW;
     Work w;
     if (!find_work<32 * NW>(a, w)) return;
-    const int64_t first = w.q0 + wave * 32;
-    const Loader<DP, NW> keys(a.k, w.k, w.kvh, a.D, wave, lane, k_pattern<DP>);
-    const Loader<DP, NW> vals(a.v, w.k, w.kvh, a.D, wave, lane, v_pattern<DP>);
-    auto issue = [&](int t) {
-        keys.load(t, lds + (t & 1) * kTileBytes);
-        vals.load(t, lds + (2 + (t & 1)) * kTileBytes);
+    const int64_t first = w.q0 + block * 32;
+    uint8_t* const mine = lds + part * 4 * kTileBytes;
+    const Loader<DP, NW> keys(a.k, w.k, w.kvh, a.D, block, lane, k_pattern<DP>);
+    const Loader<DP, NW> vals(a.v, w.k, w.kvh, a.D, block, lane, v_pattern<DP>);
+    auto issue = [&](int r) {                    // tile r KS + part
+        if (r * KS + part >= w.tiles) return;
+        keys.load(r * KS + part, mine + (r & 1) * kTileBytes);
+        vals.load(r * KS + part, mine + (2 + (r & 1)) * kTileBytes);
     };
-    if (w.tiles > 0) issue(0);
+    issue(0);
     Queries<DP, BF16> q(a, w, lane, first);
-    auto tile = [&](int t, auto masked) {
+    auto tile = [&](int r, auto masked) {
         f16v sc[2];
         typename Type<BF16>::V8 pf[4];
-        q.scores(lds + (t & 1) * kTileBytes, sc);
+        const int64_t key = (int64_t)(r * KS + part) * kTile;
+        q.scores(mine + (r & 1) * kTileBytes, sc);
         pace<DP / 16, 1, DP / 8>();
-        q.template probabilities<decltype(masked)::value>(sc, (int64_t)t * kTile, pf);
-        q.template values<decltype(masked)::value>(lds + (2 + (t & 1)) * kTileBytes, pf, (int64_t)t * kTile);
+        q.template probabilities<decltype(masked)::value>(sc, key, pf);
+        q.template values<decltype(masked)::value>(mine + (2 + (r & 1)) * kTileBytes, pf, key);
         if (!decltype(masked)::value) pace<DP / 8, 2, DP / 8>();
     };
-    auto arrived = [&](int t) {
+    auto arrived = [&](int r) {
         landed();
         meet();
-        if (t + 1 < w.tiles) issue(t + 1);
+        issue(r + 1);
     };
-    int t = 0;
-    for (; t < w.full; ++t) {
-        arrived(t);
-        tile(t, std::false_type{});
+    const int rounds = (w.tiles + KS - 1) / KS, full = w.full / KS;
+    int r = 0;
+    for (; r < full; ++r) {
+        arrived(r);
+        tile(r, std::false_type{});
     }
-    for (; t < w.tiles; ++t) {
-        arrived(t);
-        if ((int64_t)t * kTile < first + 32 + w.shift) tile(t, std::true_type{});     // (else no query of this wave sees it)
+    for (; r < rounds; ++r) {
+        arrived(r);
+        const int t = r * KS + part;             // (where no query of this wave sees it: nothing)
+        if (t < w.tiles && (int64_t)t * kTile < first + 32 + w.shift) tile(r, std::true_type{});
     }
-    q.store(a, w, first);
+    if constexpr (KS == 1) {
+        q.store(a, w, first);
+        return;
+    }
+    // Join: results 32 i .. are summed and stored by part i % KS.
+    float* const sums = reinterpret_cast<float*>(lds);
+    float* const stats = sums + NW * KS * (NV - NV / KS) * 16 * 64;
+    const float l = q.l + __shfl_xor(q.l, 32);
+    meet();
+    if (q.half == 0) stats[wave * 64 + q.col] = q.mx, stats[wave * 64 + 32 + q.col] = l;
+    meet();
+    const float* const of = stats + block * 64 + q.col;
+    float top = of[0], sum = 0.0f;
+#pragma unroll
+    for (int x = 1; x < KS; ++x) top = fmaxf(top, of[x * NW * 64]);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) sum += of[x * NW * 64 + 32] * __builtin_amdgcn_exp2f(of[x * NW * 64] - top);
+    const float down = __builtin_amdgcn_exp2f(q.mx - top);
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        q.o[i] *= down;
+        if (i % KS != part)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sums[((wave * (NV / 2) + i / 2) * 16 + e) * 64 + lane] = q.o[i][e];
+    }
+    meet();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i % KS != part) continue;
+        const int other = block + (1 - part) * NW;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) q.o[i][e] += sums[((other * (NV / 2) + i / 2) * 16 + e) * 64 + lane];
+        if (q.there) q.store_block(a, w, first, i, q.o[i], inv);
+    }
 }
 
 // NW waves on the same 32 queries, each with every NW-th tile of keys and room for one tile of its own: for calls with so few queries
@@ -466,14 +508,14 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a
     }
 }
 
-template <int DP, bool BF16, int NW>
+template <int DP, bool BF16, int NW, int KS>
 int launch_waves(PrefillArgs& a, hipStream_t st)
 {
-    constexpr size_t kLds = 4 * (size_t)kTile * DP * 2;
+    constexpr size_t kLds = KS * 4 * (size_t)kTile * DP * 2;
     static thread_local int allowed = -1;
-    if (int e = allow_large_lds(prefill_kernel<DP, BF16, NW>, kLds, allowed)) return e;
+    if (int e = allow_large_lds(prefill_kernel<DP, BF16, NW, KS>, kLds, allowed)) return e;
     a.tiles = a.q_tokens / (32 * NW) + a.sequences;
-    prefill_kernel<DP, BF16, NW><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW, kLds, st>>>(a);
+    prefill_kernel<DP, BF16, NW, KS><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW * KS, kLds, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
     return MNNQ_OK;
 }
@@ -499,10 +541,16 @@ int launch_type(PrefillArgs& a, hipStream_t st)
     // heads) 9.4 / 10.7 / 16.7; 84 (64 queries behind 2048 keys, 28 heads) 20.5 / 25.4 / 39.9; 476 16.4 / 12.7 / 18.1; 924 34.5 /
     // 23.2 / 28.4; 2080 93.9 / 65.6 / 52.3; 2296 (twenty of 100) 58.8 / 35.1 / 28.3.  (256 wide, LDS holds the tiles of two.)
     const int64_t blocks = (a.q_tokens / 32 + a.sequences) * a.heads;
-    if constexpr (DP < 256)
+    // Between one and two 128-query tiles per CU whose keys are many: those tiles, two waves on each 32 queries.  Us, against the other
+    // forms: 1200 tokens, 28 heads, 25.9 / 30.0; 1536, 32 heads, 34.3 / 37.5; 4096, 12 heads, 70 / 87; 8192, 8 heads, 146 / 179 (64 wide 89 /
+    // 110); one per CU: 8192, 4 heads, 110 / 96; more than two: 2500, 28 heads, 69 / 63; few keys: nine of 128, 32 heads, 21.8 / 13.8.
+    const int64_t wide = ((a.q_tokens + 127) / 128 + a.sequences - 1) * a.heads;
+    if constexpr (DP < 256) {
         if (blocks <= 256) return launch_split<DP, BF16, 4>(a, st);
+        if (wide > 256 && wide <= 512 && a.k_tokens >= 1024 * a.sequences) return launch_waves<DP, BF16, 4, 2>(a, st);
+    }
     if (blocks <= 1152) return launch_split<DP, BF16, 2>(a, st);
-    return launch_waves<DP, BF16, 4>(a, st);
+    return launch_waves<DP, BF16, 4, 1>(a, st);
 }
 
 template <int DP>

@@ -63,6 +63,34 @@ def test_keys_before_the_first_query(q_lens, k_lens):
           rows(gen, sum(k_lens), 2, 128, torch.bfloat16), q_lens, k_lens)
 
 
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("q_lens,k_lens", [([600], [1100]), ([1055], [1055]), ([513], [1024]), ([1, 300, 40], [2500, 300, 700]),
+                                           ([300, 260], [2000, 100])])
+def test_many_heads_and_keys(dim, dtype, q_lens, k_lens):
+    """Enough tiles of queries for every CU: two waves share the keys of a tile, one of them without any in the first rows."""
+    gen = torch.Generator().manual_seed(dim + sum(q_lens))
+    print("prompt", dim, dtype, q_lens, k_lens, flush=True)
+    check(rows(gen, sum(q_lens), 64, dim, dtype), rows(gen, sum(k_lens), 2, dim, dtype), rows(gen, sum(k_lens), 2, dim, dtype),
+          q_lens, k_lens)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["k", "v", "q"])
+def test_what_is_masked_has_no_part_with_many_heads(bad, where):
+    gen = torch.Generator().manual_seed(10)
+    n, dim, dtype, at = 1100, 64, torch.bfloat16, 555
+    x = {"q": rows(gen, n, 64, dim, dtype), "k": rows(gen, n, 1, dim, dtype), "v": rows(gen, n, 1, dim, dtype)}
+    clean = B.mnnq_attn_prefill(x["q"].cuda(), x["k"].cuda(), x["v"].cuda(), starts([n]))
+    x[where][at, :, 3] = bad
+    out = B.mnnq_attn_prefill(x["q"].cuda(), x["k"].cuda(), x["v"].cuda(), starts([n]))
+    assert torch.equal(out[:at], clean[:at])
+    if where == "q":
+        assert torch.equal(out[at + 1:], clean[at + 1:])
+    if where == "v":
+        assert not torch.isfinite(out[at:, :, 3]).any()
+
+
 def test_rows_that_see_nothing_are_zero():
     # fewer keys than queries: the first ones see none; a sequence without keys; a sequence without queries
     gen = torch.Generator().manual_seed(5)
