@@ -118,6 +118,24 @@ __device__ __forceinline__ void codes_to_float(uint32_t w, float (&v)[4])
     v[0] = (float)lo.x, v[1] = (float)lo.y, v[2] = (float)hi.x, v[3] = (float)hi.y;
 }
 
+// The last of 0 .. n - 1 for which `holds`, given that it does for none behind one that it does not for; 0 if for none.  All lanes of a wave
+// ask at once, 64 places at a time: one load's latency for up to 64 sequences where a search by halves has six
+// (200 prompts of 20 tokens, 12 heads, 34.6 -> 31.5 us; 64 of 64, 28 heads, 32.7 -> 31.6).
+template <typename Holds>
+__device__ __forceinline__ int64_t last_of(int64_t n, Holds holds)
+{
+    const int lane = __lane_id();
+    int64_t at = 0;
+    while (n > 1) {
+        const int64_t stride = (n + 63) >> 6, mine = lane * stride;
+        const uint64_t yes = __ballot(mine < n && holds(at + (mine < n ? mine : 0))) | 1;
+        const int64_t steps = (63 - __builtin_clzll(yes)) * stride;
+        at += steps;
+        n = n - steps < stride ? n - steps : stride;
+    }
+    return at;
+}
+
 // Four numbers within the codes' range as codes, ties to even.
 template <int FORM>
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)

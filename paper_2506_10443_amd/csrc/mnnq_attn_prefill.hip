@@ -126,13 +126,10 @@ __device__ __forceinline__ bool find_work(const PrefillArgs& a, Work& w)
     if (a.heads % kXcdCount == 0) w.head = w.head % kXcdCount * (a.heads / kXcdCount) + w.head / kXcdCount;
     w.kvh = w.head / (a.heads / a.kv_heads);
     // Sequence s owns the tiles from q_start[s] / BM + s on: n queries fill at most n / BM + 1.
-    int64_t lo = 0, hi = a.sequences - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        const int64_t at = a.q_start[mid], in = at < 0 ? 0 : at > a.q_tokens ? a.q_tokens : at;
-        if (in / BM + mid <= tile_id) lo = mid;
-        else hi = mid - 1;
-    }
+    const int64_t lo = last_of(a.sequences, [&](int64_t s) {
+        const int64_t at = a.q_start[s], in = at < 0 ? 0 : at > a.q_tokens ? a.q_tokens : at;
+        return in / BM + s <= tile_id;
+    });
     w.q = span_of(a.q_start, lo, a.q_tokens);
     w.k = span_of(a.k_start, lo, a.k_tokens);
     w.q0 = (tile_id - (w.q.begin / BM + lo)) * BM;

@@ -39,18 +39,12 @@ __device__ __forceinline__ bool find_piece(const AppendArgs& a, int64_t p, Piece
         n = a.each;
     } else {
         // Sequence s owns the pieces from start[s] / block + 2 s on: n tokens touch at most n / block + 2 blocks.
-        int64_t lo = 0, hi = c.sequences - 1;
         const int64_t total = a.tokens;
         auto base = [&](int64_t i) {
             const int64_t at = a.start[i];
             return (at < 0 ? 0 : at > total ? total : at) / c.block_tokens + 2 * i;
         };
-        while (lo < hi) {
-            const int64_t mid = (lo + hi + 1) >> 1;
-            if (base(mid) <= p) lo = mid;
-            else hi = mid - 1;
-        }
-        s = lo;
+        s = last_of(c.sequences, [&](int64_t i) { return base(i) <= p; });
         j = p - base(s);
         const Span span = span_of(a.start, s, total);
         begin = span.begin;
