@@ -347,11 +347,11 @@ struct Queries {
 };
 
 // NW 32-query blocks, KS waves on each with every KS-th tile of keys, the next tile in flight while one is worked on; the KS join through
-// LDS.  (KS = 1: two tiles of K and V in LDS, 64 KB at 128 wide: two
-// workgroups per CU, whose waves share the matrix cores and the vector units.  KS = 2: one workgroup, for half as many steps.)  4 D operations per visible pair and head, and as many
+// LDS.  KS = 1: two tiles of K and V in LDS, 64 KB at 128 wide, so that a CU holds two workgroups, whose waves share the matrix cores and
+// the vector units; KS = 2: one workgroup, for half as many steps.  4 D operations per visible pair and head, and as many
 // instructions on scores as matrix ones: what bounds it is the two of them by turns.  One prompt of 8192, 32 heads on 8, 128 wide:
-// 516-548 us, 1.00-1.06 PFLOP/s, matrix cores busy half of the cycles and vector issue a little less; a large matrix product
-// reaches 1.39.  Packed prompts of up to 1500 tokens, 28 heads on 4: 56 us.  64 queries a wave (half the LDS reads) spills:
+// 515-548 us, 1.00-1.07 PFLOP/s, matrix cores busy half of the cycles and vector issue a little less; a large matrix product
+// reaches 1.39.  Packed prompts of up to 1500 tokens, 28 heads on 4: 57 us.  64 queries a wave (half the LDS reads) spills:
 // 589-637; eight waves in two halves that take turns at the matrix cores: no faster.
 template <int DP, bool BF16, int NW, int KS>
 __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kernel(PrefillArgs a)

@@ -370,8 +370,8 @@ constexpr int kMoveThreads = 256;
 constexpr int kMovePieces = 4;                   // 16-byte pieces of K, and of V, that a thread has in flight
 
 // One workgroup per new block and key head.  Ranges first (the greatest of the tokens' old ones), then the codes, moved as they are
-// where old and new range agree.  A copy bounds it: 16 sequences x 8 heads of up to 4096
-// kept tokens, 128 wide, 243 MB read and written, 45-54 us = 4.5-5.3 TB/s.
+// where old and new range agree.  A copy bounds it: 16 sequences x 8 heads of up to 4096 kept tokens, 128 wide, 243 MB read
+// and written, 45-54 us = 4.5-5.3 TB/s.
 template <int KF, int VF>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
 {
