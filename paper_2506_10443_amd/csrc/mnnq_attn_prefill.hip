@@ -180,8 +180,9 @@ struct Loader {
 };
 
 // A wave's 32 queries: lane (half, col) holds of query col the scores of keys 8 i + 4 half + {0..3} of a tile and the results
-// d = 8 i + 4 half + {0..3}.
-template <int DP, bool BF16>
+// d = 8 i + 4 half + {0..3}.  DP: width of a row in LDS, DU: the part of it that products are made of (4096
+// tokens, 80 wide, 32 heads: 96 of 128 takes 120 us, all of it 136; 192 wide, 16 heads: 192 of 256 takes 143, all of it 185).
+template <int DP, int DU, bool BF16>
 struct Queries {
     using T = Type<BF16>;
     typedef typename T::V8 V8;
@@ -189,8 +190,8 @@ struct Queries {
     int64_t limit;                               // this lane's query sees the keys below
     float scale;                                 // of the scores, log2
     bool there;
-    V8 qf[DP / 16];
-    f16v o[DP / 32];
+    V8 qf[DU / 16];
+    f16v o[DU / 32];
     float mx, l;                                 // maximum of the scores times scale; sum over this lane's keys
 
     __device__ __forceinline__ Queries(const PrefillArgs& a, const Work& w, int lane, int64_t first)
@@ -201,23 +202,23 @@ struct Queries {
         limit = there ? mine + w.shift + 1 : 0;
         const uint16_t* src = a.q.data + (w.q.begin + (there ? mine : 0)) * a.q.token + w.head * a.q.head + 8 * half;
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
+        for (int i = 0; i < DU / 16; ++i) {
             u4v x = {0, 0, 0, 0};
             if (there && 16 * i + 8 * half < a.D) x = *reinterpret_cast<const u4v*>(src + 16 * i);
             qf[i] = __builtin_bit_cast(V8, x);
         }
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
+        for (int i = 0; i < DU / 32; ++i) o[i] = f16v{};
     }
 
     // S^T = K Q^T of a tile.
     __device__ __forceinline__ void scores(const uint8_t* kt, f16v (&sc)[2]) const
     {
-        V8 kf[2][DP / 16];
+        V8 kf[2][DU / 16];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
+            for (int i = 0; i < DU / 16; ++i) {
                 const int row = 32 * j + col;
                 kf[j][i] = *reinterpret_cast<const V8*>(kt + row * DP * 2 + (((2 * i + half) ^ k_pattern<DP>(row)) << 4));
             }
@@ -225,7 +226,7 @@ struct Queries {
         for (int j = 0; j < 2; ++j) {
             sc[j] = f16v{};
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) sc[j] = T::mfma(kf[j][i], qf[i], sc[j]);
+            for (int i = 0; i < DU / 16; ++i) sc[j] = T::mfma(kf[j][i], qf[i], sc[j]);
         }
     }
 
@@ -255,7 +256,7 @@ struct Queries {
             mx = now;
             l *= down;
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) o[i] *= down;
+            for (int i = 0; i < DU / 32; ++i) o[i] *= down;
         }
         const float less = T::kLift - mx;
 #pragma unroll
@@ -294,14 +295,14 @@ struct Queries {
 #pragma unroll
             for (int ks16 = 0; ks16 < 4; ++ks16)
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
+                for (int i = 0; i < DU / 32; ++i) {
                     s8v x = read_v(vt, ks16, i);
                     x = (x & 0x7fff) >= kFirst ? 0 : x;
                     o[i] = T::mfma(__builtin_bit_cast(V8, x), pf[ks16], o[i]);
                 }
             const V8 p0 = pf[0], p1 = pf[1], p2 = pf[2], p3 = pf[3];
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i)
+            for (int i = 0; i < DU / 32; ++i)
 #pragma nounroll
                 for (int j = 0; j < kTile; ++j) {
                     const V8 pj = j < 32 ? (j < 16 ? p0 : p1) : (j < 48 ? p2 : p3);
@@ -320,7 +321,7 @@ struct Queries {
 #pragma unroll
         for (int ks16 = 0; ks16 < 4; ++ks16)
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) o[i] = T::mfma(__builtin_bit_cast(V8, read_v(vt, ks16, i)), pf[ks16], o[i]);
+            for (int i = 0; i < DU / 32; ++i) o[i] = T::mfma(__builtin_bit_cast(V8, read_v(vt, ks16, i)), pf[ks16], o[i]);
     }
 
     __device__ __forceinline__ void store(const PrefillArgs& a, const Work& w, int64_t first)
@@ -329,7 +330,7 @@ struct Queries {
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         if (!there) return;
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) store_block(a, w, first, i, o[i], inv);
+        for (int i = 0; i < DU / 32; ++i) store_block(a, w, first, i, o[i], inv);
     }
 
     // Results 32 i .. 32 i + 31 of the query, times inv.
@@ -353,11 +354,11 @@ struct Queries {
 // 515-548 us, 1.00-1.07 PFLOP/s, matrix cores busy half of the cycles and vector issue a little less; a large matrix product
 // reaches 1.39.  Packed prompts of up to 1500 tokens, 28 heads on 4: 57 us.  64 queries a wave (half the LDS reads) spills:
 // 589-637; eight waves in two halves that take turns at the matrix cores: no faster.
-template <int DP, bool BF16, int NW, int KS>
+template <int DP, int DU, bool BF16, int NW, int KS>
 __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kernel(PrefillArgs a)
 {
     static_assert(KS == 1 || KS == 2);
-    constexpr int kTileBytes = kTile * DP * 2, NV = DP / 32;
+    constexpr int kTileBytes = kTile * DP * 2, NV = DU / 32;
     extern __shared__ __align__(16) uint8_t lds[];   // of each part K0 K1 V0 V1; then sums and statistics
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = wave % NW, part = wave / NW;
@@ -373,16 +374,16 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
         vals.load(r * KS + part, mine + (2 + (r & 1)) * kTileBytes);
     };
     issue(0);
-    Queries<DP, BF16> q(a, w, lane, first);
+    Queries<DP, DU, BF16> q(a, w, lane, first);
     auto tile = [&](int r, auto masked) {
         f16v sc[2];
         typename Type<BF16>::V8 pf[4];
         const int64_t key = (int64_t)(r * KS + part) * kTile;
         q.scores(mine + (r & 1) * kTileBytes, sc);
-        pace<DP / 16, 1, DP / 8>();
+        pace<DU / 16, 1, DU / 8>();
         q.template probabilities<decltype(masked)::value>(sc, key, pf);
         q.template values<decltype(masked)::value>(mine + (2 + (r & 1)) * kTileBytes, pf, key);
-        if (!decltype(masked)::value) pace<DP / 8, 2, DP / 8>();
+        if (!decltype(masked)::value) pace<DU / 8, 2, DU / 8>();
     };
     auto arrived = [&](int r) {
         landed();
@@ -406,7 +407,8 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
     }
     // Join: results 32 i .. are summed and stored by part i % KS.
     float* const sums = reinterpret_cast<float*>(lds);
-    float* const stats = sums + NW * KS * (NV - NV / KS) * 16 * 64;
+    constexpr int kSlots = (NV + 1) / 2;         // results that a wave leaves to the other one, at most
+    float* const stats = sums + NW * KS * kSlots * 16 * 64;
     const float l = q.l + __shfl_xor(q.l, 32);
     meet();
     if (q.half == 0) stats[wave * 64 + q.col] = q.mx, stats[wave * 64 + 32 + q.col] = l;
@@ -424,7 +426,7 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
         q.o[i] *= down;
         if (i % KS != part)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sums[((wave * (NV / 2) + i / 2) * 16 + e) * 64 + lane] = q.o[i][e];
+            for (int e = 0; e < 16; ++e) sums[((wave * kSlots + i / 2) * 16 + e) * 64 + lane] = q.o[i][e];
     }
     meet();
 #pragma unroll
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
         if (i % KS != part) continue;
         const int other = block + (1 - part) * NW;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) q.o[i][e] += sums[((other * (NV / 2) + i / 2) * 16 + e) * 64 + lane];
+        for (int e = 0; e < 16; ++e) q.o[i][e] += sums[((other * kSlots + i / 2) * 16 + e) * 64 + lane];
         if (q.there) q.store_block(a, w, first, i, q.o[i], inv);
     }
 }
@@ -441,10 +443,10 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
 // that tiles of queries leave CUs idle.  A wave requests its next keys when it has read the ones before, values likewise; the waves
 // join through LDS.  No barrier before the join: a wave waits for its own loads only.  Bound by that chain (load, scores, statistics,
 // values, once per NW tiles): 512 tokens, 12 heads on 2, 9.1 us with four waves; of it about 3 is what any launch takes.
-template <int DP, bool BF16, int NW>
+template <int DP, int DU, bool BF16, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a)
 {
-    constexpr int kTileBytes = kTile * DP * 2, NV = DP / 32;
+    constexpr int kTileBytes = kTile * DP * 2, NV = DU / 32;
     extern __shared__ __align__(16) uint8_t lds[];   // K and V of wave 0, of wave 1, ...; then the waves' sums and statistics
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Work w;
@@ -454,7 +456,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a
     const Loader<DP, 1> keys(a.k, w.k, w.kvh, a.D, 0, lane, k_pattern<DP>);
     const Loader<DP, 1> vals(a.v, w.k, w.kvh, a.D, 0, lane, v_pattern<DP>);
     if (wave < w.tiles) keys.load(wave, kt), vals.load(wave, vt);
-    Queries<DP, BF16> q(a, w, lane, w.q0);
+    Queries<DP, DU, BF16> q(a, w, lane, w.q0);
     auto tile = [&](int t, auto masked) {
         f16v sc[2];
         typename Type<BF16>::V8 pf[4];
@@ -505,32 +507,32 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a
     }
 }
 
-template <int DP, bool BF16, int NW, int KS>
+template <int DP, int DU, bool BF16, int NW, int KS>
 int launch_waves(PrefillArgs& a, hipStream_t st)
 {
     constexpr size_t kLds = KS * 4 * (size_t)kTile * DP * 2;
     static thread_local int allowed = -1;
-    if (int e = allow_large_lds(prefill_kernel<DP, BF16, NW, KS>, kLds, allowed)) return e;
+    if (int e = allow_large_lds(prefill_kernel<DP, DU, BF16, NW, KS>, kLds, allowed)) return e;
     a.tiles = a.q_tokens / (32 * NW) + a.sequences;
-    prefill_kernel<DP, BF16, NW, KS><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW * KS, kLds, st>>>(a);
+    prefill_kernel<DP, DU, BF16, NW, KS><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW * KS, kLds, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
     return MNNQ_OK;
 }
 
-template <int DP, bool BF16, int NW>
+template <int DP, int DU, bool BF16, int NW>
 int launch_split(PrefillArgs& a, hipStream_t st)
 {
     constexpr size_t kTiles = NW * 2 * (size_t)kTile * DP * 2, kJoin = NW * (DP * 32 + 64) * sizeof(float);
     constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
     static thread_local int allowed = -1;
-    if (int e = allow_large_lds(prefill_split_kernel<DP, BF16, NW>, kLds, allowed)) return e;
+    if (int e = allow_large_lds(prefill_split_kernel<DP, DU, BF16, NW>, kLds, allowed)) return e;
     a.tiles = a.q_tokens / 32 + a.sequences;
-    prefill_split_kernel<DP, BF16, NW><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW, kLds, st>>>(a);
+    prefill_split_kernel<DP, DU, BF16, NW><<<dim3((unsigned)(a.tiles * a.heads)), 64 * NW, kLds, st>>>(a);
     MNNQ_HIP_TRY(hipGetLastError());
     return MNNQ_OK;
 }
 
-template <int DP, bool BF16>
+template <int DP, int DU, bool BF16>
 int launch_type(PrefillArgs& a, hipStream_t st)
 {
     // By the number of 32-query blocks there may be.  Up to one per CU: four waves share a block's keys; up to four: two; else four
@@ -543,17 +545,17 @@ int launch_type(PrefillArgs& a, hipStream_t st)
     // 110); one per CU: 8192, 4 heads, 110 / 96; more than two: 2500, 28 heads, 69 / 63; few keys: nine of 128, 32 heads, 21.8 / 13.8.
     const int64_t wide = ((a.q_tokens + 127) / 128 + a.sequences - 1) * a.heads;
     if constexpr (DP < 256) {
-        if (blocks <= 256) return launch_split<DP, BF16, 4>(a, st);
-        if (wide > 256 && wide <= 512 && a.k_tokens >= 1024 * a.sequences) return launch_waves<DP, BF16, 4, 2>(a, st);
+        if (blocks <= 256) return launch_split<DP, DU, BF16, 4>(a, st);
+        if (wide > 256 && wide <= 512 && a.k_tokens >= 1024 * a.sequences) return launch_waves<DP, DU, BF16, 4, 2>(a, st);
     }
-    if (blocks <= 1152) return launch_split<DP, BF16, 2>(a, st);
-    return launch_waves<DP, BF16, 4, 1>(a, st);
+    if (blocks <= 1152) return launch_split<DP, DU, BF16, 2>(a, st);
+    return launch_waves<DP, DU, BF16, 4, 1>(a, st);
 }
 
-template <int DP>
+template <int DP, int DU>
 int launch_width(bool bf16, PrefillArgs& a, hipStream_t st)
 {
-    return bf16 ? launch_type<DP, true>(a, st) : launch_type<DP, false>(a, st);
+    return bf16 ? launch_type<DP, DU, true>(a, st) : launch_type<DP, DU, false>(a, st);
 }
 
 }  // namespace
@@ -563,8 +565,10 @@ int launch_attn_prefill(bool bf16, int64_t sequences, const int32_t* q_start, co
                         const Rows& v, const Rows& out, hipStream_t st)
 {
     PrefillArgs a{q, k, v, out, q_start, k_start, sequences, q_tokens, k_tokens, 0, heads, kv_heads, head_dim, scale * kLog2e};
-    return head_dim <= 64 ? launch_width<64>(bf16, a, st)
-         : head_dim <= 128 ? launch_width<128>(bf16, a, st) : launch_width<256>(bf16, a, st);
+    return head_dim <= 64 ? launch_width<64, 64>(bf16, a, st)
+         : head_dim <= 96 ? launch_width<128, 96>(bf16, a, st)
+         : head_dim <= 128 ? launch_width<128, 128>(bf16, a, st)
+         : head_dim <= 192 ? launch_width<256, 192>(bf16, a, st) : launch_width<256, 256>(bf16, a, st);
 }
 
 }  // namespace mnnq
