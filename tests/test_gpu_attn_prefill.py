@@ -47,6 +47,16 @@ def test_lengths_and_widths(dtype, dim, lens):
     check(rows(gen, n, 4, dim, dtype), rows(gen, n, 2, dim, dtype), rows(gen, n, 2, dim, dtype), lens, lens)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim", [48, 96, 112, 176, 192, 208])
+@pytest.mark.parametrize("heads,lens", [(2, [130]), (8, [200, 333]), (64, [600])])
+def test_widths_between_the_powers_of_two(dtype, dim, heads, lens):
+    gen = torch.Generator().manual_seed(dim + heads)
+    n = sum(lens)
+    print("prompt", dtype, dim, heads, lens, flush=True)
+    check(rows(gen, n, heads, dim, dtype), rows(gen, n, 2, dim, dtype), rows(gen, n, 2, dim, dtype), lens, lens)
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (7, 1), (8, 8), (12, 2), (28, 4)])
 def test_grouped_heads(heads, kv_heads):
     gen = torch.Generator().manual_seed(heads)
