@@ -127,7 +127,8 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
     if (p0 >= len && a.parts > 1) return;        // (one part: rows of zeros are stored)
     const int p1 = p0 + a.part_len < len ? p0 + a.part_len : len;
 
-    // The codes of a step: two tiles of 16 tokens; there: 0 where the cache has no such block.
+    // The codes of a step: two tiles of 16 tokens; there: 0 where the cache has no such block, and behind the last token, where the
+    // table's entry may name a block of anybody's or nobody's.
     struct Codes {
         bool there[2];
         u4v k[2][KC];
@@ -143,11 +144,11 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = p + 16 * i;
-            x.there[i] = (uint32_t)b.at[i] < (uint32_t)c.blocks;
+            x.there[i] = at < p1 && (uint32_t)b.at[i] < (uint32_t)c.blocks;
             const int64_t slot = (int64_t)(x.there[i] ? b.at[i] : 0) * c.kv_heads + kvh;
             // (rows behind the last token may hold anything, NaN codes among it: they are beyond the piece and come as zeros)
             const int left = p1 - at < 16 ? p1 - at : 16;
-            const int bytes = x.there[i] && left > 0 ? left * D : 0;
+            const int bytes = x.there[i] ? left * D : 0;
             const int64_t from = (slot * B + (at & (B - 1))) * D;
             const __amdgpu_buffer_rsrc_t rk = rsrc(static_cast<const uint8_t*>(c.k_codes) + from, bytes);
             const __amdgpu_buffer_rsrc_t rv = rsrc(static_cast<const uint8_t*>(c.v_codes) + from, bytes);
@@ -239,6 +240,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 }
             }
         const bool masked = p + kStep > lowest_limit || p + kStep > p1 || !x.there[0] || !x.there[1];
+        const float k0 = x.there[0] ? x.kr[0] : 0.0f, k1 = x.there[1] ? x.kr[1] : 0.0f;
         // (a range that is not finite is that of undefined values, which only rows that see them may get)
         const float v0 = x.there[0] ? x.vr[0] : 0.0f, v1 = x.there[1] ? x.vr[1] : 0.0f;
         const float vmax = fmaxf(v0 < __builtin_inff() ? v0 : 0.0f, v1 < __builtin_inff() ? v1 : 0.0f);
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                     }
                 }
             // (the factor is positive, or 0 or NaN with a range that is)
-            const float f[2] = {factor[m] * (x.kr[0] * (1.0f / code_top<KF>())), factor[m] * (x.kr[1] * (1.0f / code_top<KF>()))};
+            const float f[2] = {factor[m] * (k0 * (1.0f / code_top<KF>())), factor[m] * (k1 * (1.0f / code_top<KF>()))};
             float top = kLowest;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
