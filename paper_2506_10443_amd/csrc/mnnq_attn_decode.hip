@@ -35,7 +35,7 @@ constexpr int kOutOfRange = 0x7ffffff0;          // a byte offset beyond every p
 struct DecodeArgs {
     mnnq_kv_cache c;
     Rows q, out;
-    float* sums;                                 // [sequences, kv_heads, rows, parts, DP] where there is more than one part
+    float* means;                                // [sequences, kv_heads, rows, parts, DP] where there is more than one part
     float2* stats;                               // [sequences, kv_heads, rows, parts]: maximum (log2) and sum
     float* scores;                               // [sequences, kv_heads, rows, scores_stride] where weights are asked for
     float* weights;
@@ -358,18 +358,24 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
         float top = red_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][col]);
-        const float f = __builtin_amdgcn_exp2f(mx[m] - top) * unit * (1.0f / code_top<VF>());
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += red_l[w][col] * __builtin_amdgcn_exp2f(red_m[w][col] - top);
+        // The sum is divided out before the range comes in: a mean is no greater than what it is of, a sum may pass binary32.  (1 / all by
+        // the instruction, to one unit of fp32; a range that the quotient would bring below the normal numbers goes to the sums.)
+        float f = __builtin_amdgcn_exp2f(mx[m] - top) * (all > 0.0f || all != all ? __builtin_amdgcn_rcpf(all) : 0.0f);
+        const float range = unit * (1.0f / code_top<VF>());
+        if (unit < 0x1p-60f) {
+#pragma unroll
+            for (int i = 0; i < ND; ++i) o[m][i] *= range;
+        } else {
+            f *= range;
+        }
         const int r = row0 + m * 16 + row;
-        float rt = red_m[0][row];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) rt = fmaxf(rt, red_m[w][row]);
-        float rl = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) rl += red_l[w][row] * __builtin_amdgcn_exp2f(red_m[w][row] - rt);
-        const float inv = rl > 0.0f || rl != rl ? 1.0f / rl : 0.0f;
-        const int64_t part = ((s * c.kv_heads + kvh) * a.rows + r) * a.parts + blockIdx.x;
+        const int64_t rows = (s * c.kv_heads + kvh) * a.rows;
         const int t = r / a.group, h = kvh * a.group + r - t * a.group;
-        if (a.stats && r < a.rows && at == 0) a.stats[part] = float2{rt, rl};
+        if (a.stats && threadIdx.x < 16 && row0 + m * 16 + col < a.rows)
+            a.stats[(rows + row0 + m * 16 + col) * a.parts + blockIdx.x] = float2{top, all};
 #pragma unroll
         for (int first = 0; first < DP; first += DH) {
             if (first > 0) __syncthreads();
@@ -391,14 +397,14 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             }
             if (r >= a.rows || d >= D) continue;     // (head_dim is a multiple of a thread's values)
             if (a.parts > 1) {
-                float* to = a.sums + part * DP + d;
+                float* to = a.means + ((rows + r) * a.parts + blockIdx.x) * DP + d;
 #pragma unroll
                 for (int i = 0; i < N; ++i) to[i] = val[i];
             } else {
                 uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head + d;
 #pragma unroll
                 for (int i = 0; i < N; i += 2)
-                    *reinterpret_cast<uint32_t*>(to + i) = pack16(val[i] * inv, val[i + 1] * inv, a.bf16);
+                    *reinterpret_cast<uint32_t*>(to + i) = pack16(val[i], val[i + 1], a.bf16);
             }
         }
     }
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
 
 constexpr int kJoinThreads = 256;
 constexpr int kMaxParts = 1024;
-constexpr int kEarly = 4;                        // sums that a thread of a join requests before it knows the length
+constexpr int kEarly = 4;                        // means that a thread of a join requests before it knows the length
 constexpr int kRowsAtOnce = 64;                  // rows whose statistics a workgroup holds
 
 // Behind the parts.  Workgroups below a.rows (where there are several parts): one row's parts joined.  The others: attention
@@ -426,10 +432,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
     const int64_t s = blockIdx.z;
     const int joins = a.parts > 1 ? a.rows : 0;
     if ((int)blockIdx.x < joins) {
-        // The length and the first of the sums are requested together; what lies in parts behind the length is not looked at.
+        // The length and the first of the means are requested together; what lies in parts behind the length is not looked at.
         const int r = blockIdx.x, team = tid / PER, d = tid % PER;
         const int64_t first = ((s * c.kv_heads + kvh) * a.rows + r) * a.parts;
-        const f4v* from = reinterpret_cast<const f4v*>(a.sums + first * DP) + d;
+        const f4v* from = reinterpret_cast<const f4v*>(a.means + first * DP) + d;
         f4v early[kEarly];
 #pragma unroll
         for (int i = 0; i < kEarly; ++i) {
@@ -449,8 +455,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         float l = 0.0f;
         for (int i = tid; i < n; i += kJoinThreads) {
             const float2 st = i == tid ? mine : a.stats[first + i];
-            f[i] = __builtin_amdgcn_exp2f(st.x - top);
-            l += st.y * f[i];
+            f[i] = st.y * __builtin_amdgcn_exp2f(st.x - top);
+            l += f[i];
         }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) l += __shfl_xor(l, m);
@@ -459,19 +465,19 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         l = 0.0f;
 #pragma unroll
         for (int w = 0; w < kJoinThreads / 64; ++w) l += wave_sum[w];
+        const float inv = l > 0.0f || l != l ? __builtin_amdgcn_rcpf(l) : 0.0f;
         f4v v = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kEarly; ++i)
-            if (i * TEAMS + team < n) v += early[i] * f[i * TEAMS + team];
+            if (i * TEAMS + team < n) v += early[i] * (f[i * TEAMS + team] * inv);
 #pragma unroll 8
-        for (int i = kEarly * TEAMS + team; i < n; i += TEAMS) v += from[(int64_t)i * PER] * f[i];
+        for (int i = kEarly * TEAMS + team; i < n; i += TEAMS) v += from[(int64_t)i * PER] * (f[i] * inv);
         red[team][d] = v;
         __syncthreads();
         if (team == 0 && 4 * d < c.head_dim) {
 #pragma unroll
             for (int i = 1; i < TEAMS; ++i) v += red[i][d];
             const int t = r / a.group, h = kvh * a.group + r - t * a.group;
-            v *= l > 0.0f || l != l ? 1.0f / l : 0.0f;
             uint16_t* to = a.out.data + (s * a.tokens + t) * a.out.token + h * a.out.head;
             *reinterpret_cast<u2v*>(to + 4 * d) = u2v{pack16(v.x, v.y, a.bf16), pack16(v.z, v.w, a.bf16)};
         }
@@ -619,7 +625,7 @@ int launch_attn_decode(const mnnq_kv_cache& c, bool bf16, int64_t tokens, int he
     a.bf16 = bf16;
     const Space sp = space_of(c, p, a.rows, bound, weights != nullptr);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    a.sums = p.parts > 1 ? reinterpret_cast<float*>(ws) : nullptr;
+    a.means = p.parts > 1 ? reinterpret_cast<float*>(ws) : nullptr;
     a.stats = p.parts > 1 || weights ? reinterpret_cast<float2*>(ws + sp.stats) : nullptr;
     a.scores = weights ? reinterpret_cast<float*>(ws + sp.scores) : nullptr;
     return p.DP == 64 ? launch_width<64>(a, p, st) : p.DP == 128 ? launch_width<128>(a, p, st) : launch_width<256>(a, p, st);

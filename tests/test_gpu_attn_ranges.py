@@ -47,3 +47,16 @@ def test_entries_behind_the_last_token_may_name_any_block(n, what, dtype, k_type
     assert torch.equal(out, outs[0][0])
 
 
+@pytest.mark.parametrize("n", [1, 300, 3000])
+@pytest.mark.parametrize("v_type", [I8, F8])
+def test_values_near_the_greatest_number(n, v_type):
+    """The result is a mean of values that bfloat16 has; sums on the way must not pass it."""
+    gen = torch.Generator().manual_seed(n)
+    c = Pair(1, -(-n // 64), 1, 64, 64, I8, v_type)
+    v = (2.9e38 + 4e37 * torch.rand((n, 1, 64), generator=gen)).to(torch.bfloat16)
+    c.append(rows(gen, n, 1, 64, torch.bfloat16), v, [n])
+    q = rows(gen, 1, 4, 64, torch.bfloat16)
+    want, _ = R.decode(c.ref, c.table, [n], q, 1)
+    close(B.mnnq_attn_decode(q.cuda(), *c.args()), want, torch.bfloat16)
+
+
