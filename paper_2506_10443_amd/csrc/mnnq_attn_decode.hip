@@ -8,7 +8,9 @@
 //     [2^14, 2^15), exact down to 2^-39 of it; ranges, scale and that power are one factor per row and block applied to the
 //     fp32 sums.
 //   * V's range goes into P: p r / U, U the greatest range so far (the accumulators are rescaled when it grows).  Probabilities
-//     stay below 2^14 instead of 1, so that a half holds them down to 2^-32 of the greatest.
+//     stay below 2^14 instead of 1, so that a half holds them down to 2^-32 of the greatest, 2^-28 with the least r / U.  Where a wave
+//     meets ranges 16 times below U, or U comes to 16 times its first, a great range says nothing about a row (its attention there may be none, its codes zeros, its
+//     limit before): P then stays as it is, with a power of two per row and half step, and r / U multiplies the fp32 products.
 // A wave takes 32 tokens at a time, with the codes of its next 32 in flight; the waves of a workgroup share a part of the
 // sequence and join through LDS, the parts are joined by a second kernel.
 //
@@ -18,6 +20,8 @@
 // through LDS: each code is used by one lane.
 #include "mnnq_attn.h"
 #include "mnnq_forms.h"
+
+#include <type_traits>
 
 namespace mnnq {
 
@@ -30,6 +34,7 @@ constexpr float kSlack = 6.0f;                   // the running maximum follows 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLeastNormal = 1.17549435e-38f;
+constexpr float kNear = 1.0f / 16;               // the least r / U that goes into P
 constexpr int kOutOfRange = 0x7ffffff0;          // a byte offset beyond every piece: loads give 0
 
 struct DecodeArgs {
@@ -213,6 +218,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
     f4v o[MT][ND];
     float mx[MT], l[MT];
     float unit = 0.0f, inv_unit = 0.0f;          // U and 1 / U
+    float first_unit = __builtin_inff();         // the first U
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         mx[m] = kLowest;
@@ -221,7 +227,73 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
         for (int i = 0; i < ND; ++i) o[m][i] = f4v{0, 0, 0, 0};
     }
 
-    auto step = [&](int p, const Codes& x) {
+    // V: a byte of four tokens each, twice
+    auto values_of = [&](const Codes& x, int w, int b) {
+        half8v vf;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            half2v lo, hi;
+            byte_to_half<VF>(x.v[4 * i][w], x.v[4 * i + 1][w], x.v[4 * i + 2][w], x.v[4 * i + 3][w], b, lo, hi);
+            vf[4 * i] = lo.x, vf[4 * i + 1] = lo.y, vf[4 * i + 2] = hi.x, vf[4 * i + 3] = hi.y;
+        }
+        return vf;
+    };
+    // A step's products with V, ranges far apart: a pass for each half step, one for both where they share a range.
+    struct Seen {
+        float pr[8];
+        uint32_t hidden;
+    };
+    auto add_apart = [&](Codes& x, const Seen (&seen)[MT], float v0, float v1) {
+        const bool both = v0 == v1;
+#pragma nounroll
+        for (int half = 0; half < (both ? 1 : 2); ++half) {
+            const float v = half ? v1 : v0;
+            if (v == 0.0f) continue;
+            const bool number = v < __builtin_inff();
+            half8v ph[MT];
+            float back[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                float mine[8], top = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    mine[i] = both || i / 4 == half ? seen[m].pr[i] : 0.0f;
+                    top = fmaxf(top, mine[i]);
+                }
+                // the row's greatest to [2^13, 2^14); a range that is no number, to the rows that see it, as it is
+                const uint32_t up = min(267u - (__float_as_uint(column_max(top)) >> 23), 253u);
+                const float mul = number ? __uint_as_float(up << 23) : v;
+                back[m] = number ? v * inv_unit * __uint_as_float((254u - up) << 23) : 1.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    mine[i] = seen[m].hidden >> i & 1 || (!both && i / 4 != half) ? 0.0f : mine[i] * mul;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const half2v h = __builtin_bit_cast(half2v, pack16(mine[2 * e], mine[2 * e + 1], false));
+                    ph[m][2 * e] = h.x, ph[m][2 * e + 1] = h.y;
+                }
+            }
+            // (the codes as new ones: their halves are not kept over the passes, which would take more registers than there are)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int w = 0; w < VW; ++w) asm volatile("" : "+v"(x.v[i][w]));
+#pragma unroll
+            for (int w = 0; w < VW; ++w)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const half8v vf = values_of(x, w, b);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        o[m][4 * w + b] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, ph[m], f4v{0, 0, 0, 0}, 0, 0, 0) * back[m];
+                }
+        }
+    };
+
+    // A step whose ranges call for the other form hides all of its tokens and ends the loop: a branch out of it costs more (131072
+    // tokens, 33.5 us: 34.4 with one behind the scores, 36 with one in front of them).
+    int end = p1;
+    auto step = [&](int p, Codes& x, auto apart) {
         f4v sc[MT][2];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -239,20 +311,27 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                     sc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[m][2 * j + 1], sc[m][i], 0, 0, 0);
                 }
             }
-        const bool masked = p + kStep > lowest_limit || p + kStep > p1 || !x.there[0] || !x.there[1];
         const float k0 = x.there[0] ? x.kr[0] : 0.0f, k1 = x.there[1] ? x.kr[1] : 0.0f;
         // (a range that is not finite is that of undefined values, which only rows that see them may get)
         const float v0 = x.there[0] ? x.vr[0] : 0.0f, v1 = x.there[1] ? x.vr[1] : 0.0f;
-        const float vmax = fmaxf(v0 < __builtin_inff() ? v0 : 0.0f, v1 < __builtin_inff() ? v1 : 0.0f);
         float less_unit = 1.0f;                  // what the accumulators take of U's growth
-        if (vmax > unit) {
-            const float now = fmaxf(vmax, kLeastNormal);
-            less_unit = unit / now;
-            unit = now;
-            inv_unit = 1.0f / now;
+        if (!(fmaxf(v0, v1) <= unit && fminf(v0, v1) >= unit * kNear)) {
+            // (a zero, and what is no number, have no say)
+            const bool n0 = v0 > 0.0f && v0 < __builtin_inff(), n1 = v1 > 0.0f && v1 < __builtin_inff();
+            const float vmax = fmaxf(n0 ? v0 : 0.0f, n1 ? v1 : 0.0f), now = fmaxf(vmax, unit), low = now * kNear;
+            if (!decltype(apart)::value && ((n0 && v0 < low) || (n1 && v1 < low) || first_unit < low)) {
+                end = p;
+            } else if (vmax > unit) {
+                first_unit = fminf(first_unit, vmax);
+                less_unit = unit / fmaxf(vmax, kLeastNormal);
+                unit = fmaxf(vmax, kLeastNormal);
+                inv_unit = 1.0f / unit;
+            }
         }
         const float ratio[2] = {v0 * inv_unit, v1 * inv_unit};
+        const bool masked = p + kStep > lowest_limit || p + kStep > end || !x.there[0] || !x.there[1];
         half8v pf[MT];
+        Seen seen[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             uint32_t hidden = 0;
@@ -260,7 +339,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int t = p + 16 * (i / 4) + 4 * g + (i & 3);
-                    if (t >= limit[m] || t >= p1 || !x.there[i / 4]) {
+                    if (t >= limit[m] || t >= end || !x.there[i / 4]) {
                         hidden |= 1u << i;
                         sc[m][i / 4][i & 3] = -__builtin_inff();
                     }
@@ -302,6 +381,12 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 for (int i = 0; i < 8; ++i)
                     if (hidden >> i & 1) pr[i] = 0.0f;
             l[m] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+            if constexpr (decltype(apart)::value) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) seen[m].pr[i] = pr[i];
+                seen[m].hidden = hidden;
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) pr[i] *= ratio[i / 4];
             if (masked)                              // (a ratio that is no number is not theirs)
@@ -314,36 +399,40 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 pf[m][2 * e] = h.x, pf[m][2 * e + 1] = h.y;
             }
         }
-        // V: a byte of four tokens each, twice
+        if constexpr (decltype(apart)::value) {
+            add_apart(x, seen, v0, v1);
+            return;
+        }
 #pragma unroll
         for (int w = 0; w < VW; ++w)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                half8v vf;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    half2v lo, hi;
-                    byte_to_half<VF>(x.v[4 * i][w], x.v[4 * i + 1][w], x.v[4 * i + 2][w], x.v[4 * i + 3][w], b, lo, hi);
-                    vf[4 * i] = lo.x, vf[4 * i + 1] = lo.y, vf[4 * i + 2] = hi.x, vf[4 * i + 3] = hi.y;
-                }
+                const half8v vf = values_of(x, w, b);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     o[m][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[m], o[m][4 * w + b], 0, 0, 0);
             }
     };
 
-    for (; p < p1; p += 2 * kStride) {
+    for (; p < end; p += 2 * kStride) {
         const int q = p + kStride;
         arrived(x0, ahead);
         if (q < p1) load(q, ahead, x1);
         ahead = find(q + kStride);
-        step(p, x0);
-        if (q >= p1) break;
+        step(p, x0, std::false_type{});
+        if (q >= end) break;
         arrived(x1, ahead);
         if (q + kStride < p1) load(q + kStride, ahead, x0);
         ahead = find(q + 2 * kStride);
-        step(q, x1);
+        step(q, x1, std::false_type{});
     }
+    // (a step's codes when it needs them, so that its products have the registers)
+    p = end, end = p1;
+    if (__builtin_expect(p < p1, 0))
+        for (; p < p1; p += kStride) {
+            load(p, find(p), x0);
+            step(p, x0, std::true_type{});
+        }
 
     // Join the waves: lane (g, col) holds of row col the values d = VB (4 g + v) + i, v = 0..3.
     const int row = threadIdx.x / (4 * kWaves), at = threadIdx.x % (4 * kWaves);
