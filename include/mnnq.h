@@ -317,7 +317,7 @@ int mnnq_plan_debug(int what, int64_t M, int64_t N, int64_t K, int group, int mo
  * Heads.  heads is a multiple of kv_heads; query head h reads key and value head h / (heads / kv_heads).
  * head_dim: a multiple of 16, 16 to 256.  scale: the factor of q . k (usually 1 / sqrt(head_dim)), finite
  * and above zero.
- * A query that no key is visible to gives a row of zeros.  Softmax statistics and sums are fp32; the
+ * A query that no key is visible to gives a row of zeros; one whose visible scores are all -inf gives NaN (0 / 0).  Softmax statistics and sums are fp32; the
  * probabilities enter the second product rounded to the type of its other operand (prompt: `type`,
  * cache: fp16, where those below 2^-32 of the row's greatest are lost), the result is rounded once.
  * A NaN or an infinity in q, k or v reaches the rows that see it and no other row.

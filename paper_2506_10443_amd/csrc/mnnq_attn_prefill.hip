@@ -324,10 +324,12 @@ struct Queries {
             for (int i = 0; i < DU / 32; ++i) o[i] = T::mfma(__builtin_bit_cast(V8, read_v(vt, ks16, i)), pf[ks16], o[i]);
     }
 
+    // 1 / sum.  A row that sees keys and has a sum of zero has scores of -inf only: 0 / 0, and not the zeros of a row that sees none.
+    __device__ __forceinline__ float inverse(float sum) const { return limit > 0 ? 1.0f / sum : 0.0f; }
+
     __device__ __forceinline__ void store(const PrefillArgs& a, const Work& w, int64_t first)
     {
-        const float sum = l + __shfl_xor(l, 32);
-        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+        const float inv = inverse(l + __shfl_xor(l, 32));
         if (!there) return;
 #pragma unroll
         for (int i = 0; i < DU / 32; ++i) store_block(a, w, first, i, o[i], inv);
@@ -420,7 +422,7 @@ __global__ __launch_bounds__(64 * NW * KS, DP == 256 ? 1 : 2) void prefill_kerne
 #pragma unroll
     for (int x = 0; x < KS; ++x) sum += of[x * NW * 64 + 32] * __builtin_amdgcn_exp2f(of[x * NW * 64] - top);
     const float down = __builtin_amdgcn_exp2f(q.mx - top);
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float inv = q.inverse(sum);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         q.o[i] *= down;
@@ -494,7 +496,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_split_kernel(PrefillArgs a
 #pragma unroll
         for (int e = 0; e < 16; ++e) sums[((wave * NV + i) * 16 + e) * 64 + lane] = q.o[i][e] * down;
     meet();
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float inv = q.inverse(sum);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (i % NW != wave) continue;
