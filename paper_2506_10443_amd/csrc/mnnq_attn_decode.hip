@@ -41,7 +41,7 @@ struct DecodeArgs {
     mnnq_kv_cache c;
     Rows q, out;
     float* means;                                // [sequences, kv_heads, rows, parts, DP] where there is more than one part
-    float2* stats;                               // [sequences, kv_heads, rows, parts]: maximum (log2) and sum
+    float2* stats;                               // [sequences, kv_heads, rows, parts]: maximum (log2; -inf: no key) and sum
     float* scores;                               // [sequences, kv_heads, rows, scores_stride] where weights are asked for
     float* weights;
     int64_t tokens, scores_stride, weights_stride;
@@ -217,6 +217,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
 
     f4v o[MT][ND];
     float mx[MT], l[MT];
+    int earliest = p1;                           // first token of the wave's, in sixteens, that is there
     float unit = 0.0f, inv_unit = 0.0f;          // U and 1 / U
     float first_unit = __builtin_inff();         // the first U
 #pragma unroll
@@ -238,12 +239,8 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
         }
         return vf;
     };
-    // A step's products with V, ranges far apart: a pass for each half step, one for both where they share a range.
-    struct Seen {
-        float pr[8];
-        uint32_t hidden;
-    };
-    auto add_apart = [&](Codes& x, const Seen (&seen)[MT], float v0, float v1) {
+    // A step's products with V, ranges far apart: a pass for each half step, one for both where they share a range.  P: -0 where hidden.
+    auto add_apart = [&](Codes& x, const float (&pr)[MT][8], float v0, float v1) {
         const bool both = v0 == v1;
 #pragma nounroll
         for (int half = 0; half < (both ? 1 : 2); ++half) {
@@ -257,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 float mine[8], top = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    mine[i] = both || i / 4 == half ? seen[m].pr[i] : 0.0f;
+                    mine[i] = both || i / 4 == half ? pr[m][i] : -0.0f;
                     top = fmaxf(top, mine[i]);
                 }
                 // the row's greatest to [2^13, 2^14); a range that is no number, to the rows that see it, as it is
@@ -265,8 +262,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 const float mul = number ? __uint_as_float(up << 23) : v;
                 back[m] = number ? v * inv_unit * __uint_as_float((254u - up) << 23) : 1.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    mine[i] = seen[m].hidden >> i & 1 || (!both && i / 4 != half) ? 0.0f : mine[i] * mul;
+                for (int i = 0; i < 8; ++i) mine[i] = __float_as_uint(mine[i]) >> 31 ? 0.0f : mine[i] * mul;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const half2v h = __builtin_bit_cast(half2v, pack16(mine[2 * e], mine[2 * e + 1], false));
@@ -329,9 +325,10 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             }
         }
         const float ratio[2] = {v0 * inv_unit, v1 * inv_unit};
+        earliest = min(earliest, x.there[0] ? p : x.there[1] ? p + 16 : p1);
         const bool masked = p + kStep > lowest_limit || p + kStep > end || !x.there[0] || !x.there[1];
         half8v pf[MT];
-        Seen seen[MT];
+        float all_pr[MT][8];                     // (ranges apart)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             uint32_t hidden = 0;
@@ -383,8 +380,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             l[m] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
             if constexpr (decltype(apart)::value) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) seen[m].pr[i] = pr[i];
-                seen[m].hidden = hidden;
+                for (int i = 0; i < 8; ++i) all_pr[m][i] = hidden >> i & 1 ? -0.0f : pr[i];
                 continue;
             }
 #pragma unroll
@@ -400,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             }
         }
         if constexpr (decltype(apart)::value) {
-            add_apart(x, seen, v0, v1);
+            add_apart(x, all_pr, v0, v1);
             return;
         }
 #pragma unroll
@@ -442,17 +438,20 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (m > 0) __syncthreads();
-        if (g == 0) red_m[wave][col] = mx[m], red_l[wave][col] = sum;
+        // (a row without a key has a maximum of -inf; one that sees keys of -inf only the lowest number, and 0 / 0 in the end)
+        if (g == 0) red_m[wave][col] = earliest < p1 && earliest < limit[m] ? mx[m] : -__builtin_inff(), red_l[wave][col] = sum;
         __syncthreads();
         float top = red_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][col]);
+        const float base = fmaxf(top, kLowest);
         float all = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += red_l[w][col] * __builtin_amdgcn_exp2f(red_m[w][col] - top);
+        for (int w = 0; w < kWaves; ++w) all += red_l[w][col] * __builtin_amdgcn_exp2f(red_m[w][col] - base);
         // The sum is divided out before the range comes in: a mean is no greater than what it is of, a sum may pass binary32.  (1 / all by
         // the instruction, to one unit of fp32; a range that the quotient would bring below the normal numbers goes to the sums.)
-        float f = __builtin_amdgcn_exp2f(mx[m] - top) * (all > 0.0f || all != all ? __builtin_amdgcn_rcpf(all) : 0.0f);
+        const bool divide = a.parts > 1 ? all > 0.0f || all != all : top >= kLowest;      // (of several parts another may have what is divided by)
+        float f = __builtin_amdgcn_exp2f(mx[m] - base) * (divide ? __builtin_amdgcn_rcpf(all) : 0.0f);
         const float range = unit * (1.0f / code_top<VF>());
         if (unit < 0x1p-60f) {
 #pragma unroll
@@ -533,7 +532,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         }
         const float2 mine = a.stats[first + (tid < a.parts ? tid : 0)];
         const int n = (length_of(a, s) + a.part_len - 1) / a.part_len;
-        float top = tid < n ? mine.x : kLowest;
+        float top = tid < n ? mine.x : -__builtin_inff();
         for (int i = tid + kJoinThreads; i < n; i += kJoinThreads) top = fmaxf(top, a.stats[first + i].x);
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
@@ -541,10 +540,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kJoinThreads / 64; ++w) top = fmaxf(top, wave_top[w]);
+        const float base = fmaxf(top, kLowest);
         float l = 0.0f;
         for (int i = tid; i < n; i += kJoinThreads) {
             const float2 st = i == tid ? mine : a.stats[first + i];
-            f[i] = st.y * __builtin_amdgcn_exp2f(st.x - top);
+            f[i] = st.y * __builtin_amdgcn_exp2f(st.x - base);
             l += f[i];
         }
 #pragma unroll
@@ -554,7 +554,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         l = 0.0f;
 #pragma unroll
         for (int w = 0; w < kJoinThreads / 64; ++w) l += wave_sum[w];
-        const float inv = l > 0.0f || l != l ? __builtin_amdgcn_rcpf(l) : 0.0f;
+        const float inv = top >= kLowest ? __builtin_amdgcn_rcpf(l) : 0.0f;
         f4v v = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kEarly; ++i)
@@ -584,17 +584,18 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         for (int r = tid / 16; r < rows; r += kJoinThreads / 16) {
             const float2* st = a.stats + (row0 + base + r) * a.parts;
             const int i0 = tid & 15;
-            const float2 mine = i0 < n ? st[i0] : float2{kLowest, 0.0f};
+            const float2 mine = i0 < n ? st[i0] : float2{-__builtin_inff(), 0.0f};
             float top = mine.x;
             for (int i = i0 + 16; i < n; i += 16) top = fmaxf(top, st[i].x);
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-            float l = mine.y * __builtin_amdgcn_exp2f(mine.x - top);
-            for (int i = i0 + 16; i < n; i += 16) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - top);
+            const float base = fmaxf(top, kLowest);
+            float l = mine.y * __builtin_amdgcn_exp2f(mine.x - base);
+            for (int i = i0 + 16; i < n; i += 16) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - base);
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) l += __shfl_xor(l, m);
             // (a row that sees nothing gives nothing)
-            if (i0 == 0) row_top[r] = top - kTopBits, row_inv[r] = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            if (i0 == 0) row_top[r] = base - kTopBits, row_inv[r] = top >= kLowest ? 1.0f / l : 0.0f;
         }
         __syncthreads();
         if (t < len) {

@@ -52,3 +52,37 @@ def test_prompt_rows_that_see_nothing_beside_them():
     agrees(B.mnnq_attn_prefill(q.cuda(), k.cuda(), v.cuda(), starts([40]), starts([30])), want, torch.float16)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("k_type,v_type", [(I8, F8), (F8, I8)])
+@pytest.mark.parametrize("lengths,dim", [([1, 40, 3], 64), ([300, 17, 0], 256), ([2600, 700, 1], 64)])
+def test_cache_rows_of_infinite_scores(dtype, k_type, v_type, lengths, dim):
+    """One wave, several, several parts; two queries each, of which the first sees nothing where there is one token."""
+    gen = torch.Generator().manual_seed(sum(lengths))
+    c = filled(gen, [0] * len(lengths), 2, 64, dim, k_type, v_type, extra=-(-max(lengths) // 64))
+    n = sum(lengths)
+    k = rows(gen, n, 2, dim, dtype)
+    k[:, :, 3] = k[:, :, 3].abs() + 0.5                     # (a code of at least one step in every token)
+    c.append(k, rows(gen, n, 2, dim, dtype), lengths)
+    q = rows(gen, 2 * len(lengths), 8, dim, dtype)
+    q[:, 1, 3] = q[3, 6, 3] = float("-inf")
+    want, want_w = R.decode(c.ref, c.table, lengths, q, 2)
+    w = torch.zeros((len(lengths), 2, c.table.shape[1] * 64), device="cuda")
+    agrees(B.mnnq_attn_decode(q.cuda(), *c.args()), want, dtype)
+    agrees(B.mnnq_attn_decode(q.cuda(), *c.args(), weights=w), want, dtype)
+    got = w[..., :max(lengths)].cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want_w))
+    assert R.error(got.nan_to_num(0.0), want_w.nan_to_num(0.0)) <= 1e-5
+
+
+def test_a_cache_without_any_of_its_blocks_gives_zeros():
+    gen = torch.Generator().manual_seed(4)
+    for n in (40, 900):
+        c = filled(gen, [n], 1, 16, 64)
+        table = torch.full_like(c.table, -1)
+        w = torch.zeros((1, 1, table.shape[1] * 16), device="cuda")
+        for q in (rows(gen, 1, 4, 64, torch.float16), torch.full((1, 4, 64), float("-inf"), dtype=torch.float16)):
+            assert not B.mnnq_attn_decode(q.cuda(), *c.args(table=table)).any()
+            assert not B.mnnq_attn_decode(q.cuda(), *c.args(table=table), weights=w).any()
+        assert not w.any()
+
+
