@@ -350,14 +350,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             if (a.scores && row0 + m * 16 + col < a.rows) {
                 float* to = a.scores + ((s * c.kv_heads + kvh) * a.rows + row0 + m * 16 + col) * a.scores_stride + p + 4 * g;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    f4v z = sc[m][i] * f[i];
-                    if (masked)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (hidden >> (4 * i + e) & 1) z[e] = -__builtin_inff();
-                    *reinterpret_cast<f4v*>(to + 16 * i) = z;
-                }
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<f4v*>(to + 16 * i) = sc[m][i] * f[i];      // (what is hidden is not looked at)
             }
             top = column_max(top);
             const bool follow = __ballot(top > mx[m] + kSlack) != 0;
@@ -514,6 +507,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
     __shared__ float wave_top[kJoinThreads / 64], wave_sum[kJoinThreads / 64];
     __shared__ f4v red[TEAMS][PER];
     __shared__ float row_top[kRowsAtOnce], row_inv[kRowsAtOnce];
+    __shared__ int row_limit[kRowsAtOnce];       // the row sees the tokens below
     const mnnq_kv_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int kvh = blockIdx.y;
@@ -573,16 +567,18 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
         return;
     }
     const int len = length_of(a, s), n = (len + a.part_len - 1) / a.part_len;
-    const int64_t t0 = (int64_t)((int)blockIdx.x - joins) * kJoinThreads, t = t0 + tid;
+    const int t0 = ((int)blockIdx.x - joins) * kJoinThreads, t = t0 + tid;
     if (t0 >= len) return;
+    const int32_t block = t < len ? c.block_table[s * c.table_blocks + (t >> __builtin_ctz(c.block_tokens))] : -1;
     const int64_t row0 = (s * c.kv_heads + kvh) * a.rows;
     float sum = 0.0f;
-    for (int base = 0; base < a.rows; base += kRowsAtOnce) {
-        const int rows = a.rows - base < kRowsAtOnce ? a.rows - base : kRowsAtOnce;
+    for (int first = 0; first < a.rows; first += kRowsAtOnce) {
+        const int rows = a.rows - first < kRowsAtOnce ? a.rows - first : kRowsAtOnce;
         __syncthreads();
         // sixteen lanes per row
         for (int r = tid / 16; r < rows; r += kJoinThreads / 16) {
-            const float2* st = a.stats + (row0 + base + r) * a.parts;
+            const int limit = len - (int)a.tokens + (first + r) / a.group + 1;
+            const float2* st = a.stats + (row0 + first + r) * a.parts;
             const int i0 = tid & 15;
             const float2 mine = i0 < n ? st[i0] : float2{-__builtin_inff(), 0.0f};
             float top = mine.x;
@@ -594,17 +590,23 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a)
             for (int i = i0 + 16; i < n; i += 16) l += st[i].y * __builtin_amdgcn_exp2f(st[i].x - base);
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) l += __shfl_xor(l, m);
-            // (a row that sees nothing gives nothing)
-            if (i0 == 0) row_top[r] = base - kTopBits, row_inv[r] = top >= kLowest ? 1.0f / l : 0.0f;
+            if (i0 == 0) {
+                row_top[r] = top - kTopBits;
+                row_inv[r] = 1.0f / l;
+                row_limit[r] = limit;
+            }
         }
         __syncthreads();
         if (t < len) {
-            const float* from = a.scores + (row0 + base) * a.scores_stride + t;
+            const float* from = a.scores + (row0 + first) * a.scores_stride + t;
 #pragma unroll 8
-            for (int r = 0; r < rows; ++r) sum += __builtin_amdgcn_exp2f(from[r * a.scores_stride] - row_top[r]) * row_inv[r];
+            for (int r = 0; r < rows; ++r) {
+                const float p = __builtin_amdgcn_exp2f(from[r * a.scores_stride] - row_top[r]) * row_inv[r];
+                sum += t < row_limit[r] ? p : 0.0f;      // (by its place: a row that is no number would give NaN also to what it does not see)
+            }
         }
     }
-    if (t < len) a.weights[(s * c.kv_heads + kvh) * a.weights_stride + t] += sum;
+    if ((uint32_t)block < (uint32_t)c.blocks) a.weights[(s * c.kv_heads + kvh) * a.weights_stride + t] += sum;
 }
 
 struct Plan {
