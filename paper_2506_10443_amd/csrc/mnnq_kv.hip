@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
     }
     for (int i = tid; i < last; i += kSelectThreads) {
         kept[places + i] = old + i;
-        nw[places + i] = w[old + i];
+        nw[places + i] = weight_of(weight_key(w[old + i]));
     }
     for (int64_t i = n + tid; i < a.keep; i += kSelectThreads) kept[i] = -1;
     for (int64_t i = n + tid; i < a.new_weights_stride; i += kSelectThreads) nw[i] = 0.0f;

@@ -1,0 +1,37 @@
+"""mnnq_kv_evict: tokens whose blocks the cache does not have, weights shorter than a sequence, the newest tokens' weights."""
+import pytest
+import torch
+
+import attn_reference as R
+from paper_2506_10443_amd import binding as B
+from test_gpu_attn_decode import TOL
+from test_gpu_kv_cache import F8, I8, Pair, rows, sums
+
+pytestmark = pytest.mark.gpu
+
+
+def chosen(w, there, keep, recent):
+    """Places kept of a row of weights, `there` the places that can be."""
+    newest = there[len(there) - min(recent, keep, len(there)):]
+    others = there[:len(there) - len(newest)]
+    best = sorted(others, key=lambda i: (-float(w[i]), i))[:min(keep, len(there)) - len(newest)]
+    return sorted(best) + newest
+
+def test_the_newest_tokens_weights_are_written_like_the_others():
+    """-0 as 0, every NaN as the same one."""
+    gen = torch.Generator().manual_seed(4)
+    c = Pair(1, 4, 1, 16, 16, I8, I8, spare=2)
+    k = rows(gen, 60, 1, 16, torch.float16)
+    c.append(k, k, [60])
+    w = torch.full((1, 1, 64), -0.0)
+    odd = torch.tensor([0x7f800001, -1, 0x7fc00000, -0x80000000], dtype=torch.int64).to(torch.int32).view(torch.float32)
+    w[0, 0, 10:14] = odd
+    w[0, 0, 56:60] = odd
+    nw = torch.empty((1, 1, 20), device="cuda")
+    kept, _ = B.mnnq_kv_evict(*c.args(), w.cuda(), 20, 8, c.free.view(1, 2).cuda(), nw)
+    places = kept[0, 0].tolist()
+    assert places == list(range(9)) + [10, 11, 12] + list(range(52, 60))
+    bits = nw[0, 0].cpu().view(torch.int32).tolist()
+    assert bits == [0x7fc00000 if p in (10, 11, 12, 56, 57, 58) else 0 for p in places]
+
+
