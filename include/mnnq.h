@@ -395,7 +395,8 @@ int mnnq_attn_decode(const mnnq_kv_cache *cache, int type, int64_t tokens, int h
  * greatest weights (among equal ones the earlier; NaN counts as greatest), min(keep, length) in all, and
  * writes them, in their order, to the blocks of new_table [sequences, new_table_blocks] of the same cache.
  * Those blocks must not be among the blocks the sequences hold now, which afterwards are free.
- * weights: fp32 [sequences, kv_heads, weights_stride], as mnnq_attn_decode adds them up.
+ * weights: fp32 [sequences, kv_heads, weights_stride], as mnnq_attn_decode adds them up; tokens behind them have a
+ * weight of zero.
  * A new block's range is the greatest range that its tokens' blocks had; codes are rounded to it.
  * kept: int32 [sequences, kv_heads, keep], the kept tokens' old places, -1 behind the last; new_lengths:
  * int32 [sequences]; new_weights: fp32 [sequences, kv_heads, new_weights_stride], the kept tokens' weights

@@ -219,7 +219,6 @@ __device__ __forceinline__ int64_t evict_length(const EvictArgs& a, int64_t s)
     const int64_t room = a.c.table_blocks * a.c.block_tokens;
     int64_t len = a.c.lengths[s];
     len = len > room ? room : len;
-    len = len > a.weights_stride ? a.weights_stride : len;
     return len < 0 ? 0 : len;
 }
 
@@ -247,25 +246,27 @@ __device__ __forceinline__ float weight_of(uint32_t key)
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits[3] = {11, 11, 10};         // bits of a key that a pass settles, from the top
 
+struct SelectSpace {
+    int hist[2048];
+    int wave_sum[kSelectWaves], wave_equal[kSelectWaves], wave_above[kSelectWaves];
+    uint32_t digit;
+    int need;
+};
+
 // One workgroup per sequence and key head: the key of the last token that is kept by a radix search of three passes over the
 // keys, then the kept tokens in order.  Wave w has the tokens from w * per_wave on, 64 at a time; R: keys that a thread holds (0: they
 // are read again in every pass).  Comparing keys pairwise or sorting them would cost more than the three counts of n; one
 // workgroup, since each pass waits for the one before: 4097 tokens 10.7 us, 16 x 8 rows of 16000 21.9, both the chain of barriers
 // and additions to LDS counters, at under a tenth of the rate of memory.
 template <int R>
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
+__device__ __forceinline__ void select_row(const EvictArgs& a, SelectSpace& sh, int64_t s, int head, int len)
 {
     constexpr int kUnroll = R > 0 ? R : 1;
-    __shared__ int hist[2048];
-    __shared__ int wave_sum[kSelectWaves], wave_equal[kSelectWaves], wave_above[kSelectWaves];
-    __shared__ uint32_t sh_digit;
-    __shared__ int sh_need;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int head = blockIdx.x;
-    const int64_t s = blockIdx.y;
-    const int len = (int)evict_length(a, s), n = (int)evict_kept(a, len);
+    const int n = (int)evict_kept(a, len);
     const int64_t row = s * a.c.kv_heads + head;
     const float* w = a.weights + row * a.weights_stride;
+    const int weights = a.weights_stride < len ? (int)a.weights_stride : len;      // tokens behind them have a weight of zero
     int32_t* kept = a.kept + row * a.keep;
     float* nw = a.new_weights + row * a.new_weights_stride;
     const int last = a.recent < n ? (int)a.recent : n;       // kept as the newest
@@ -274,7 +275,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
     const int steps = (len + kSelectThreads - 1) / kSelectThreads, first = wave * steps * 64 + lane;
     const int most = R > 0 ? R : steps;                      // (a bound that loops over held keys are unrolled by)
     // (0: no token that competes; the keys of numbers and NaN are above it)
-    auto key_at = [&](int j) { return first + j * 64 < old ? weight_key(w[first + j * 64]) : 0u; };
+    auto weight_at = [&](int i) { return i < weights ? w[i] : 0.0f; };
+    auto key_at = [&](int j) { return first + j * 64 < old ? weight_key(weight_at(first + j * 64)) : 0u; };
     uint32_t held[kUnroll];
     if (R > 0)
 #pragma unroll
@@ -291,37 +293,37 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
         for (int pass = 0; pass < 3; ++pass) {
             const int bits = kDigits[pass], above = shift;
             shift -= bits;
-            for (int i = tid; i < 2048; i += kSelectThreads) hist[i] = 0;
+            for (int i = tid; i < 2048; i += kSelectThreads) sh.hist[i] = 0;
             __syncthreads();
             const uint32_t settled = pass == 0 ? 0u : prefix >> above, mask = (1u << bits) - 1;
 #pragma unroll kUnroll
             for (int j = 0; j < most; ++j) {
                 if (j >= steps) continue;
                 const uint32_t key = key_of(j);
-                if (key && (pass == 0 || key >> above == settled)) atomicAdd(&hist[key >> shift & mask], 1);
+                if (key && (pass == 0 || key >> above == settled)) atomicAdd(&sh.hist[key >> shift & mask], 1);
             }
             __syncthreads();
             // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
-            const int b0 = hist[2047 - 2 * tid], b1 = hist[2046 - 2 * tid];
+            const int b0 = sh.hist[2047 - 2 * tid], b1 = sh.hist[2046 - 2 * tid];
             int sum = b0 + b1;
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1) {
                 const int other = __shfl_up(sum, m);
                 if (lane >= m) sum += other;
             }
-            if (lane == 63) wave_sum[wave] = sum;
+            if (lane == 63) sh.wave_sum[wave] = sum;
             __syncthreads();
             int before = sum - b0 - b1;
 #pragma unroll
-            for (int x = 0; x < kSelectWaves; ++x) before += x < wave ? wave_sum[x] : 0;
+            for (int x = 0; x < kSelectWaves; ++x) before += x < wave ? sh.wave_sum[x] : 0;
             if (before < need && before + b0 + b1 >= need) {
                 const bool second = before + b0 < need;
-                sh_digit = 2047 - 2 * tid - (second ? 1 : 0);
-                sh_need = need - before - (second ? b0 : 0);
+                sh.digit = 2047 - 2 * tid - (second ? 1 : 0);
+                sh.need = need - before - (second ? b0 : 0);
             }
             __syncthreads();
-            prefix |= sh_digit << shift;
-            need = sh_need;
+            prefix |= sh.digit << shift;
+            need = sh.need;
         }
     }
     // Kept: the keys above the prefix, of those that equal it the first `need`, and the newest tokens behind them.
@@ -332,12 +334,12 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
         n_above += __popcll(__ballot(key_of(j) > prefix));
         n_equal += __popcll(__ballot(key_of(j) == prefix));
     }
-    if (lane == 0) wave_above[wave] = n_above, wave_equal[wave] = n_equal;
+    if (lane == 0) sh.wave_above[wave] = n_above, sh.wave_equal[wave] = n_equal;
     __syncthreads();
     int at = 0, equal_before = 0;
 #pragma unroll
     for (int x = 0; x < kSelectWaves; ++x)
-        if (x < wave) at += wave_above[x], equal_before += wave_equal[x];
+        if (x < wave) at += sh.wave_above[x], equal_before += sh.wave_equal[x];
     at += equal_before < need ? equal_before : need;
     at = __builtin_amdgcn_readfirstlane(at), equal_before = __builtin_amdgcn_readfirstlane(equal_before);
     auto below = [](uint64_t m) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); };
@@ -359,11 +361,21 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
     }
     for (int i = tid; i < last; i += kSelectThreads) {
         kept[places + i] = old + i;
-        nw[places + i] = weight_of(weight_key(w[old + i]));
+        nw[places + i] = weight_of(weight_key(weight_at(old + i)));
     }
     for (int64_t i = n + tid; i < a.keep; i += kSelectThreads) kept[i] = -1;
     for (int64_t i = n + tid; i < a.new_weights_stride; i += kSelectThreads) nw[i] = 0.0f;
     if (head == 0 && tid == 0) a.new_lengths[s] = n;
+}
+
+template <int R>
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
+{
+    __shared__ SelectSpace sh;
+    const int len = (int)evict_length(a, blockIdx.y);
+    // (R is chosen by the room that weights and table have, whichever is less: a sequence may be longer than its weights)
+    if (R > 0 && len > R * kSelectThreads) select_row<0>(a, sh, blockIdx.y, blockIdx.x, len);
+    else select_row<R>(a, sh, blockIdx.y, blockIdx.x, len);
 }
 
 constexpr int kMoveThreads = 256;

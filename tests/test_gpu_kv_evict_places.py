@@ -35,3 +35,23 @@ def test_the_newest_tokens_weights_are_written_like_the_others():
     assert bits == [0x7fc00000 if p in (10, 11, 12, 56, 57, 58) else 0 for p in places]
 
 
+@pytest.mark.parametrize("n", [200, 5000])
+@pytest.mark.parametrize("stride", [1, 100, 150])
+def test_weights_shorter_than_the_sequence(n, stride):
+    """Tokens behind the weights have a weight of zero; the newest ones stay."""
+    gen = torch.Generator().manual_seed(n + stride)
+    c = Pair(1, n // 16 + 1, 2, 16, 16, I8, I8, spare=4)
+    k = rows(gen, n, 2, 16, torch.float16)
+    c.append(k, k, [n])
+    w = sums(gen, (1, 2, stride))
+    whole = torch.cat([w, torch.zeros(1, 2, n - stride)], -1)
+    for keep, recent in ((60, 20), (64, 0), (5, 5)):
+        nw = torch.empty((1, 2, 64), device="cuda")
+        kept, left = B.mnnq_kv_evict(*c.args(), w.cuda(), keep, recent, c.free.view(1, 4).cuda(), nw)
+        assert left.tolist() == [keep]
+        for h in range(2):
+            places = chosen(whole[0, h], list(range(n)), keep, recent)
+            assert kept[0, h].tolist() == places
+            assert torch.equal(nw[0, h, :keep].cpu(), whole[0, h][torch.tensor(places)]) and not nw[0, h, keep:].any()
+
+
