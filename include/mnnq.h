@@ -394,6 +394,7 @@ int mnnq_attn_decode(const mnnq_kv_cache *cache, int type, int64_t tokens, int h
 /* Keeps, of every sequence and key head by itself, the last `recent` tokens and those of the others with the
  * greatest weights (among equal ones the earlier; NaN counts as greatest), min(keep, length) in all, and
  * writes them, in their order, to the blocks of new_table [sequences, new_table_blocks] of the same cache.
+ * Tokens in blocks that the cache does not have are dropped, as if the sequence had none of them.
  * Those blocks must not be among the blocks the sequences hold now, which afterwards are free.
  * weights: fp32 [sequences, kv_heads, weights_stride], as mnnq_attn_decode adds them up; tokens behind them have a
  * weight of zero.

@@ -222,11 +222,15 @@ __device__ __forceinline__ int64_t evict_length(const EvictArgs& a, int64_t s)
     return len < 0 ? 0 : len;
 }
 
-__device__ __forceinline__ int64_t evict_kept(const EvictArgs& a, int64_t len)
+// Whether the cache has the block of a sequence's token.
+__device__ __forceinline__ bool token_there(const EvictArgs& a, int64_t s, int token)
 {
-    const int64_t room = a.new_table_blocks * a.c.block_tokens;
-    const int64_t n = len < a.keep ? len : a.keep;
-    return n < room ? n : room;
+    return (uint32_t)a.c.block_table[s * a.c.table_blocks + (token >> __builtin_ctz(a.c.block_tokens))] < (uint32_t)a.c.blocks;
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t mask)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
 // Floats in the order of their values as unsigned integers; NaN above all, both zeros the same.
@@ -243,14 +247,20 @@ __device__ __forceinline__ float weight_of(uint32_t key)
     return __uint_as_float(key == 0xffffffffu ? 0x7fc00000u : key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
+// Of a token: zero behind the weights.
+__device__ __forceinline__ float weight_at(const EvictArgs& a, int64_t row, int token)
+{
+    return token < a.weights_stride ? a.weights[row * a.weights_stride + token] : 0.0f;
+}
+
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits[3] = {11, 11, 10};         // bits of a key that a pass settles, from the top
 
 struct SelectSpace {
     int hist[2048];
-    int wave_sum[kSelectWaves], wave_equal[kSelectWaves], wave_above[kSelectWaves];
+    __align__(16) int wave_sum[kSelectWaves], wave_equal[kSelectWaves], wave_above[kSelectWaves];
     uint32_t digit;
-    int need;
+    int need, old;
 };
 
 // One workgroup per sequence and key head: the key of the last token that is kept by a radix search of three passes over the
@@ -258,43 +268,67 @@ struct SelectSpace {
 // are read again in every pass).  Comparing keys pairwise or sorting them would cost more than the three counts of n; one
 // workgroup, since each pass waits for the one before: 4097 tokens 10.7 us, 16 x 8 rows of 16000 21.9, both the chain of barriers
 // and additions to LDS counters, at under a tenth of the rate of memory.
-template <int R>
-__device__ __forceinline__ void select_row(const EvictArgs& a, SelectSpace& sh, int64_t s, int head, int len)
+// `missing` of the tokens are in blocks that the cache does not have, which are masked everywhere and kept nowhere: GAPS.
+// raw: the weights of a thread's R tokens.
+template <int R, bool GAPS>
+__device__ __forceinline__ void select_row(const EvictArgs& a, SelectSpace& sh, int64_t s, int head, int len, int missing,
+                                           const float (&raw)[R > 0 ? R : 1])
 {
+    static_assert(!(R > 0 && GAPS));
     constexpr int kUnroll = R > 0 ? R : 1;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n = (int)evict_kept(a, len);
+    const int64_t room = a.new_table_blocks * a.c.block_tokens, most_kept = a.keep < room ? a.keep : room;
+    const int n = len - missing < most_kept ? len - missing : (int)most_kept;
     const int64_t row = s * a.c.kv_heads + head;
-    const float* w = a.weights + row * a.weights_stride;
-    const int weights = a.weights_stride < len ? (int)a.weights_stride : len;      // tokens behind them have a weight of zero
     int32_t* kept = a.kept + row * a.keep;
     float* nw = a.new_weights + row * a.new_weights_stride;
     const int last = a.recent < n ? (int)a.recent : n;       // kept as the newest
-    const int old = len - last;                              // the others compete
+    int old = len - last;                                    // the others compete
+    if (GAPS) {                                              // (those of the last that are there, counted from the end)
+        if (wave == 0) {
+            int found = 0;
+            old = len;
+            while (found < last && old > 0) {                // (there are at least n)
+                const int token = old - 64 + lane;
+                uint64_t some = __ballot(token >= 0 && token_there(a, s, token >= 0 ? token : 0));
+                found += __popcll(some);
+                for (; found > last; --found) some &= some - 1;
+                old = found < last ? old - 64 : old - 64 + __builtin_ctzll(some);
+            }
+            if (lane == 0) sh.old = old < 0 ? 0 : old;
+        }
+        __syncthreads();
+        old = sh.old;
+    }
+    const int competing = len - missing - last;
     const int places = n - last;                             // for this many places
     const int steps = (len + kSelectThreads - 1) / kSelectThreads, first = wave * steps * 64 + lane;
     const int most = R > 0 ? R : steps;                      // (a bound that loops over held keys are unrolled by)
     // (0: no token that competes; the keys of numbers and NaN are above it)
-    auto weight_at = [&](int i) { return i < weights ? w[i] : 0.0f; };
-    auto key_at = [&](int j) { return first + j * 64 < old ? weight_key(weight_at(first + j * 64)) : 0u; };
+    auto key_at = [&](int j) {
+        const int token = first + j * 64;
+        return token < old && (!GAPS || token_there(a, s, token)) ? weight_key(weight_at(a, row, token)) : 0u;
+    };
     uint32_t held[kUnroll];
     if (R > 0)
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) held[j] = j < steps ? key_at(j) : 0u;
+        for (int j = 0; j < kUnroll; ++j) held[j] = j < steps && first + j * 64 < old ? weight_key(raw[j]) : 0u;
     auto key_of = [&](int j) { return R > 0 ? held[R > 0 ? j : 0] : key_at(j); };
 
     // prefix: the settled bits of the last kept key; need: places left for keys that have them.  All keys are above 0, none above
     // the greatest.
     uint32_t prefix = places > 0 ? 0u : 0xffffffffu;
     int need = 0;
-    if (places > 0 && places < old) {
+    if (places > 0 && places < competing) {
         need = places;
         int shift = 32;
         for (int pass = 0; pass < 3; ++pass) {
             const int bits = kDigits[pass], above = shift;
             shift -= bits;
-            for (int i = tid; i < 2048; i += kSelectThreads) sh.hist[i] = 0;
-            __syncthreads();
+            if (pass > 0) {                      // (for the first one they are zero)
+                for (int i = tid; i < 2048; i += kSelectThreads) sh.hist[i] = 0;
+                __syncthreads();
+            }
             const uint32_t settled = pass == 0 ? 0u : prefix >> above, mask = (1u << bits) - 1;
 #pragma unroll kUnroll
             for (int j = 0; j < most; ++j) {
@@ -342,16 +376,15 @@ __device__ __forceinline__ void select_row(const EvictArgs& a, SelectSpace& sh, 
         if (x < wave) at += sh.wave_above[x], equal_before += sh.wave_equal[x];
     at += equal_before < need ? equal_before : need;
     at = __builtin_amdgcn_readfirstlane(at), equal_before = __builtin_amdgcn_readfirstlane(equal_before);
-    auto below = [](uint64_t m) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); };
 #pragma unroll kUnroll
     for (int j = 0; j < most; ++j) {
         if (j >= steps) continue;
         const uint32_t key = key_of(j);
         bool take = key > prefix;
         const uint64_t eq = __ballot(key == prefix);
-        if (eq && equal_before < need) take |= key == prefix && equal_before + below(eq) < need;
+        if (eq && equal_before < need) take |= key == prefix && equal_before + lanes_below(eq) < need;
         const uint64_t tk = __ballot(take);
-        const int to = at + below(tk);
+        const int to = at + lanes_below(tk);
         if (take && to < n) {
             kept[to] = first + j * 64;
             nw[to] = weight_of(key);
@@ -359,9 +392,23 @@ __device__ __forceinline__ void select_row(const EvictArgs& a, SelectSpace& sh, 
         equal_before += __popcll(eq);
         at += __popcll(tk);
     }
-    for (int i = tid; i < last; i += kSelectThreads) {
-        kept[places + i] = old + i;
-        nw[places + i] = weight_of(weight_key(weight_at(old + i)));
+    if (!GAPS) {
+        for (int i = tid; i < last; i += kSelectThreads) {
+            kept[places + i] = old + i;
+            nw[places + i] = weight_of(weight_key(weight_at(a, row, old + i)));
+        }
+    } else if (wave == 0) {
+        int to = places;
+        for (int token = old + lane; token - lane < len; token += 64) {
+            const bool there = token < len && token_there(a, s, token < len ? token : 0);
+            const uint64_t some = __ballot(there);
+            const int place = to + lanes_below(some);
+            if (there && place < n) {
+                kept[place] = token;
+                nw[place] = weight_of(weight_key(weight_at(a, row, token)));
+            }
+            to += __popcll(some);
+        }
     }
     for (int64_t i = n + tid; i < a.keep; i += kSelectThreads) kept[i] = -1;
     for (int64_t i = n + tid; i < a.new_weights_stride; i += kSelectThreads) nw[i] = 0.0f;
@@ -372,10 +419,33 @@ template <int R>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 {
     __shared__ SelectSpace sh;
-    const int len = (int)evict_length(a, blockIdx.y);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.c.block_tokens;
+    const int64_t s = blockIdx.y;
+    const int head = blockIdx.x, len = (int)evict_length(a, s);
+    const int steps = (len + kSelectThreads - 1) / kSelectThreads;
+    // (weights and table are requested together)
+    float raw[R > 0 ? R : 1];
+    if (R > 0)
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+            raw[j] = j < steps ? weight_at(a, s * a.c.kv_heads + head, wave * steps * 64 + j * 64 + lane) : 0.0f;
+    int missing = 0;
+    for (int64_t first = (int64_t)tid * B; first < len; first += (int64_t)kSelectThreads * B)
+        if (!token_there(a, s, (int)first)) missing += len - (int)first < B ? len - (int)first : B;
+    if (__ballot(missing != 0))
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) missing += __shfl_xor(missing, m);
+    if (lane == 0) sh.wave_sum[wave] = missing;
+    for (int i = tid; i < 2048; i += kSelectThreads) sh.hist[i] = 0;
+    __syncthreads();
+    missing = 0;
+#pragma unroll
+    for (int x = 0; x < kSelectWaves; ++x) missing += sh.wave_sum[x];
     // (R is chosen by the room that weights and table have, whichever is less: a sequence may be longer than its weights)
-    if (R > 0 && len > R * kSelectThreads) select_row<0>(a, sh, blockIdx.y, blockIdx.x, len);
-    else select_row<R>(a, sh, blockIdx.y, blockIdx.x, len);
+    const float none[1] = {0.0f};
+    if (missing > 0) select_row<0, true>(a, sh, s, head, len, missing, none);
+    else if (R > 0 && steps > R) select_row<0, false>(a, sh, s, head, len, 0, none);
+    else select_row<R, false>(a, sh, s, head, len, 0, raw);
 }
 
 constexpr int kMoveThreads = 256;
@@ -396,17 +466,15 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
     // (the length, the new block and the first of the places are requested together)
     const int32_t early = tid < B && b * B + tid < a.keep ? kept[tid] : -1;
     const int64_t to = a.new_table[s * a.new_table_blocks + b];
-    const int64_t left = evict_kept(a, evict_length(a, s)) - b * B;
+    const int64_t left = a.new_lengths[s] - b * B;
     if (left <= 0 || to < 0 || to >= a.c.blocks) return;
     const int count = (int)(left < B ? left : B);
-    // where each token lies, and its ranges
+    // where each token lies (in a block that the cache has: the others were not kept), and its ranges
     if (tid < count) {
-        const int64_t block = a.c.block_table[s * a.c.table_blocks + early / B];
-        const bool there = block >= 0 && block < a.c.blocks;
-        const int64_t at = (there ? block : 0) * a.c.kv_heads + head;
-        from[tid] = there ? (at * B + early % B) * D : -1;
-        range_of[0][tid] = there ? a.c.k_range[at] : 0.0f;
-        range_of[1][tid] = there ? a.c.v_range[at] : 0.0f;
+        const int64_t at = (int64_t)a.c.block_table[s * a.c.table_blocks + early / B] * a.c.kv_heads + head;
+        from[tid] = (at * B + early % B) * D;
+        range_of[0][tid] = a.c.k_range[at];
+        range_of[1][tid] = a.c.v_range[at];
     }
     __syncthreads();
     // (magnitudes as integers; a NaN stays one)
@@ -430,7 +498,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a)
             const int at = base + i * kMoveThreads;
             r[i] = at < pieces ? at / per_row : -1;
             k[i] = v[i] = uint4{0, 0, 0, 0};
-            if (r[i] >= 0 && from[r[i]] >= 0) {
+            if (r[i] >= 0) {
                 const int64_t source = from[r[i]] + (at - r[i] * per_row) * 16;
                 k[i] = *reinterpret_cast<const uint4*>(codes[0] + source);
                 v[i] = *reinterpret_cast<const uint4*>(codes[1] + source);
