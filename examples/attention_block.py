@@ -18,6 +18,9 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2506_10443_amd import binding as B, synth  # noqa: E402
 
 
+PROMPT_QUERIES = 32     # of a prompt that goes to eviction: how many of the last ones say what was attended to
+
+
 class Blocks:
     """A pool of cache blocks and the blocks that nobody holds."""
 
@@ -79,7 +82,11 @@ class AttentionBlock:
         return B.mnnq_linear_prefill_f16_o16(self.o, self.hidden, a.shape[1], a)
 
     def prompt(self, x, counts):
-        """x fp16 [sum of counts, hidden], the sequences' prompts one behind the other."""
+        """x fp16 [sum of counts, hidden], the sequences' prompts one behind the other; the cache is empty."""
+        if self.longest:
+            raise RuntimeError("prompt attention looks at the prompt only: the cache must be empty")
+        if max(counts) > self.table.shape[1] * self.pool.block_tokens:
+            raise RuntimeError("a sequence has no room for its prompt")
         starts = [0]
         for n in counts:
             starts.append(starts[-1] + n)
@@ -89,8 +96,19 @@ class AttentionBlock:
         self.lengths += start[1:] - start[:-1]
         self.longest += max(counts)
         out = self.output(B.mnnq_attn_prefill(q, k, v, start))
-        self.evict()
+        if self.beyond_budget():
+            self.account(q, starts)
+            self.evict()
         return out
+
+    def account(self, q, starts):
+        """Prompt attention keeps no account: a prompt that is beyond the budget at once is judged by the attention that its last
+        queries give, asked of the cache again."""
+        for s in range(len(starts) - 1):
+            first, last = max(starts[s], starts[s + 1] - PROMPT_QUERIES), starts[s + 1]
+            if last > first:
+                B.mnnq_attn_decode(q[first:last], *self.pool.arrays(), self.table[s:s + 1], self.lengths[s:s + 1],
+                                   max_length=last - starts[s], weights=self.given[s:s + 1])
 
     def step(self, x):
         """x fp16 [sequences, hidden]: one token of every sequence."""
@@ -105,10 +123,14 @@ class AttentionBlock:
         self.evict()
         return out
 
+    def beyond_budget(self):
+        """Whether the longest sequence is a block beyond it."""
+        return self.budget is not None and self.longest >= self.budget + self.pool.block_tokens
+
     def evict(self):
-        """Back to the budget when the longest sequence is a block beyond it."""
+        """Back to the budget where it is exceeded."""
         block = self.pool.block_tokens
-        if self.budget is None or self.longest < self.budget + block:
+        if not self.beyond_budget():
             return None
         need = -(-self.budget // block)
         fresh = [self.pool.take(need) for _ in self.held]
