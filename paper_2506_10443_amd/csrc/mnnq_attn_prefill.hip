@@ -35,7 +35,7 @@ template <>
 struct Type<true> {
     typedef bf8v V8;
     static __device__ __forceinline__ f16v mfma(V8 a, V8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-    static constexpr float kLift = 0.0f;
+    static constexpr float kLift = -16.0f;       // probabilities from 2^-16 down: sums of the greatest values stay numbers
     // l + the two values of a dword, which are summed as the second product uses them: rounded.  One instruction in place of two
     // additions (packed prompts of up to 1500 tokens, 28 heads, 64 -> 58 us).
     static __device__ __forceinline__ float add_pair(uint32_t two, float l)
