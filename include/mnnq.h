@@ -317,9 +317,11 @@ int mnnq_plan_debug(int what, int64_t M, int64_t N, int64_t K, int group, int mo
  * Heads.  heads is a multiple of kv_heads; query head h reads key and value head h / (heads / kv_heads).
  * head_dim: a multiple of 16, 16 to 256.  scale: the factor of q . k (usually 1 / sqrt(head_dim)), finite
  * and above zero.
- * A query that no key is visible to gives a row of zeros; one whose visible scores are all -inf gives NaN (0 / 0).  Softmax statistics and sums are fp32; the
+ * A query that no key is visible to gives a row of zeros; one whose visible scores are all -inf gives
+ * NaN (0 / 0).  Scores (one beyond fp32 is an infinity), softmax statistics and sums are fp32; the
  * probabilities enter the second product rounded to the type of its other operand (prompt: `type`,
- * cache: fp16, where those below 2^-32 of the row's greatest are lost), the result is rounded once.
+ * cache: fp16, where those below 2^-28 of the row's greatest are lost), the result is rounded once.
+ * `out` must not overlap q, k, v or the cache.
  * A NaN or an infinity in q, k or v reaches the rows that see it and no other row.
  * Device arrays of indices are not looked at on the host; what they hold is bounded in the kernels: a
  * sequence's start and end are clamped to the number of rows given (an end before its start is an empty
@@ -381,8 +383,8 @@ int mnnq_kv_append(const mnnq_kv_cache *cache, int type, const int32_t *start, i
  * sequences are cut to their first max_length tokens.  The work is laid out for max_length, so that one not
  * far above the longest length is the fastest.
  * weights: NULL, or fp32 [sequences, kv_heads, weights_stride], weights_stride >= the bound: the attention
- * given to token j by all queries that share the head, sum_{queries, heads of the group} softmax_j, is added
- * to weights[s, h, j].
+ * given to token j by all queries that share the head and see it, sum_{queries, heads of the group} softmax_j,
+ * is added to weights[s, h, j].
  * workspace: mnnq_attn_decode_workspace_size() bytes, 16-byte aligned, scratch; calls sharing one must not
  * overlap in time.  NULL where the size is 0. */
 size_t mnnq_attn_decode_workspace_size(const mnnq_kv_cache *cache, int64_t tokens, int heads, int64_t max_length,

@@ -5,19 +5,20 @@
 // into the lanes of one column, where the next product wants its probabilities: the four scores of a lane in two tiles of 16
 // tokens are its eight values of P^T as they stand.
 //   * Codes become halves exactly; bfloat16 queries become halves scaled by a power of two per row so that the greatest is in
-//     [2^14, 2^15), exact down to 2^-39 of it; ranges, scale and that power are one factor per row and block applied to the
-//     fp32 sums.
+//     [2^14, 2^15), exact down to 2^-31 of it, below that to 2^-39 of it; ranges, scale and that power are one factor per row and
+//     block applied to the fp32 sums.
 //   * V's range goes into P: p r / U, U the greatest range so far (the accumulators are rescaled when it grows).  Probabilities
 //     stay below 2^14 instead of 1, so that a half holds them down to 2^-32 of the greatest, 2^-28 with the least r / U.  Where a wave
-//     meets ranges 16 times below U, or U comes to 16 times its first, a great range says nothing about a row (its attention there may be none, its codes zeros, its
-//     limit before): P then stays as it is, with a power of two per row and half step, and r / U multiplies the fp32 products.
+//     meets ranges 16 times below U, or U comes to 16 times its first, a great range says nothing about a row: it may have no attention
+//     there, codes of zero, or end before.  P then stays as it is, under a power of two per row and half step, and r / U multiplies the
+//     fp32 products.
 // A wave takes 32 tokens at a time, with the codes of its next 32 in flight; the waves of a workgroup share a part of the
 // sequence and join through LDS, the parts are joined by a second kernel.
 //
 // 2 D bytes per token and key head are read once and 4 D rows operations done with them, at most a few dozen per byte: HBM bounds long
-// caches, a chain of launch, ramp and join short ones.  One token (both kernels): 131072 tokens of 4 key heads, 134 MB, 33.3 us, 28 of
-// them the first kernel at 4.8 TB/s (its loads alone 25.5); 32 ragged sequences, 178 MB, 45; 1001 tokens 8.4.  Loads go to registers, not
-// through LDS: each code is used by one lane.
+// caches, a chain of launch, ramp and join short ones.  One token (both kernels): 131072 tokens of 4 key heads, 134 MB, 34.1 us, 29 of
+// them the first kernel at 4.6 TB/s (its loads alone 25.5); 32 ragged sequences, 178 MB, 45.6; 1001 tokens 8.9.  Ranges far apart: 131072
+// tokens 42.7, in blocks of 16 tokens 51.6.  Loads go to registers, not through LDS: each code is used by one lane.
 #include "mnnq_attn.h"
 #include "mnnq_forms.h"
 
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
             top = column_max(top);
             const bool follow = __ballot(top > mx[m] + kSlack) != 0;
             if (follow || less_unit != 1.0f) {
-                const float now = top > mx[m] + kSlack ? top : mx[m];        // (each row by itself: its bits do not depend on the others)
+                const float now = top > mx[m] + kSlack ? top : mx[m];        // (each row by itself)
                 const float down = __builtin_amdgcn_exp2f(mx[m] - now);
                 mx[m] = now;
                 l[m] *= down;

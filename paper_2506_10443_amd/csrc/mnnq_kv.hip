@@ -266,8 +266,8 @@ struct SelectSpace {
 // One workgroup per sequence and key head: the key of the last token that is kept by a radix search of three passes over the
 // keys, then the kept tokens in order.  Wave w has the tokens from w * per_wave on, 64 at a time; R: keys that a thread holds (0: they
 // are read again in every pass).  Comparing keys pairwise or sorting them would cost more than the three counts of n; one
-// workgroup, since each pass waits for the one before: 4097 tokens 10.7 us, 16 x 8 rows of 16000 21.9, both the chain of barriers
-// and additions to LDS counters, at under a tenth of the rate of memory.
+// workgroup, since each pass waits for the one before: 4097 tokens 11.9 us, 16 x 8 rows of up to 16315 16.3, both the chain of
+// barriers and additions to LDS counters, at under a tenth of the rate of memory.
 // `missing` of the tokens are in blocks that the cache does not have, which are masked everywhere and kept nowhere: GAPS.
 // raw: the weights of a thread's R tokens.
 template <int R, bool GAPS>
