@@ -150,8 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = p + 16 * i;
-            x.there[i] = at < p1 && (uint32_t)b.at[i] < (uint32_t)c.blocks;
-            const int64_t slot = (int64_t)(x.there[i] ? b.at[i] : 0) * c.kv_heads + kvh;
+            const bool known = (uint32_t)b.at[i] < (uint32_t)c.blocks;
+            x.there[i] = known & (at < p1);
+            const int64_t slot = (int64_t)(known ? b.at[i] : 0) * c.kv_heads + kvh;
             // (rows behind the last token may hold anything, NaN codes among it: they are beyond the piece and come as zeros)
             const int left = p1 - at < 16 ? p1 - at : 16;
             const int bytes = x.there[i] ? left * D : 0;
@@ -320,9 +321,10 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
                 end = p;
             } else if (vmax > unit) {
                 first_unit = fminf(first_unit, vmax);
-                less_unit = unit / fmaxf(vmax, kLeastNormal);
+                const float before = unit;
                 unit = fmaxf(vmax, kLeastNormal);
                 inv_unit = 1.0f / unit;
+                less_unit = before * inv_unit;
             }
         }
         const float ratio[2] = {v0 * inv_unit, v1 * inv_unit};
