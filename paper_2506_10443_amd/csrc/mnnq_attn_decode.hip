@@ -16,9 +16,9 @@
 // sequence and join through LDS, the parts are joined by a second kernel.
 //
 // 2 D bytes per token and key head are read once and 4 D rows operations done with them, at most a few dozen per byte: HBM bounds long
-// caches, a chain of launch, ramp and join short ones.  One token (both kernels): 131072 tokens of 4 key heads, 134 MB, 34.1 us, 29 of
-// them the first kernel at 4.6 TB/s (its loads alone 25.5); 32 ragged sequences, 178 MB, 45.6; 1001 tokens 8.9.  Ranges far apart: 131072
-// tokens 42.7, in blocks of 16 tokens 51.6.  Loads go to registers, not through LDS: each code is used by one lane.
+// caches, a chain of launch, ramp and join short ones.  One token (both kernels): 131072 tokens of 4 key heads, 134 MB, 33.6 us, 29 of
+// them the first kernel at 4.6 TB/s (its loads alone 25.5); 32 ragged sequences, 178 MB, 45.3; 1001 tokens 8.6.  Ranges far apart: 131072
+// tokens 41.2, in blocks of 16 tokens 50.1.  Loads go to registers, not through LDS: each code is used by one lane.
 #include "mnnq_attn.h"
 #include "mnnq_forms.h"
 
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void decode_kernel(
     };
 
     // A step whose ranges call for the other form hides all of its tokens and ends the loop: a branch out of it costs more (131072
-    // tokens, 33.5 us: 34.4 with one behind the scores, 36 with one in front of them).
+    // tokens, 33.9 us: 34.4 with one behind the scores, 36 with one in front of them).
     int end = p1;
     auto step = [&](int p, Codes& x, auto apart) {
         f4v sc[MT][2];
